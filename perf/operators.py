@@ -16,6 +16,7 @@ own = False
 DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
 THETA = 1e6                # base of the rotation's frequencies
 CELLS = 169                # tokens of a 13 x 13 frame, the grid of most videos here
+ROWS_OF_FRAME = 82         # what the merge leaves of such a frame at half the tokens
 EPS = 1e-6
 DECAY = 0.95               # what a running score keeps of itself per step
 
@@ -46,7 +47,7 @@ def listed():
         dict(at, name="attend_5338", len=5338),
         # the same over the longest video, collecting the weights for an eviction
         dict(at, name="attend_55788_scored", len=55788, scored=True),
-        # questions on parts of videos: half of the slots masked, ragged lengths, 64-channel heads
+        # questions on parts of videos: half of the frames masked, ragged lengths, 64-channel heads
         dict(at, name="attend_24_ragged_masked", dtype="f16", q_heads=14, kv_heads=2, dim=64, page=16, seqs=24, len=21013, spread=0.9, masked=0.5),
         # a full serving batch with weights collected
         dict(big, op="attend", name="attend_32_long_scored", seqs=32, len=32700, spread=0.1, masked=0.0, scored=True, page=32, order="slots"),
@@ -169,7 +170,11 @@ def prepare(c, seed):
         s["lengths"] = torch.tensor(n, dtype=torch.int32, device=dev)
         # unit-variance logits, with a few heads that look at little
         s["q"] = torch.randn((S, H, D), generator=gen, device=dev).mul_(torch.rand((S, H, 1), generator=gen, device=dev) * 2 + 0.3).to(dt)
-        s["mask"] = (torch.rand((S, max(n)), generator=gen, device=dev) >= c["masked"]) if c["masked"] else None
+        # a question on part of a video leaves out whole frames: runs of the rows that the merge leaves of one
+        s["mask"] = None
+        if c["masked"]:
+            frames = torch.rand((S, max(n) // ROWS_OF_FRAME + 1), generator=gen, device=dev) >= c["masked"]
+            s["mask"] = frames.repeat_interleave(ROWS_OF_FRAME, 1)[:, :max(n)].contiguous()
         s["scores"] = torch.rand((S, K, max(n)), generator=gen, device=dev) * 1e-2 if c["scored"] else None
     else:
         s["k_pages"], s["v_pages"], s["table"] = pool(c, n, gen, dev, True)
