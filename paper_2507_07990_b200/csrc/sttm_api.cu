@@ -11,6 +11,7 @@
 #include <cstring>
 #include <vector>
 
+#include "sttm_host.cuh"
 #include "sttm_kernels.cuh"
 #include "sttm_fused.cuh"
 #include "sttm_flow.cuh"
@@ -21,21 +22,6 @@
 namespace {
 
 using namespace sttm;
-
-constexpr int kSmCount = 148;   // B200 (grid sizes of the older kernels; the streaming kernels ask the device)
-
-// multiprocessors of the current device
-int sm_count() {
-    static int cached[64] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return kSmCount;
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = kSmCount;
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
 
 thread_local int g_launches = 0;
 // What the budget mode hands to its two passes of the ordinary path (nothing of it is global state).
@@ -70,17 +56,6 @@ inline void mark_stage(int boundary, cudaStream_t st) {
         nvtxRangePushA(kStageNames[g_last_path][boundary]);
         g_range_open = true;
     }
-}
-
-inline size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
-
-// index of the current device for the per-device tables below (function attributes and occupancy
-// answers belong to a device); -1 when it cannot be had or is beyond the tables
-constexpr int kMaxDevices = 64;
-inline int device_slot() {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
-    return dev;
 }
 
 // Launch shape of the fused kernel for one problem; ok == false: the three-pass kernels run.
@@ -539,12 +514,6 @@ sttm_status by_levels_dtype(int L, sttm_dtype dt, F&& f) {
     return f(std::integral_constant<int, 3>{}, (const float*)nullptr);
 }
 
-#define STTM_CUDA_TRY(expr)                          \
-    do {                                             \
-        cudaError_t e_ = (expr);                     \
-        if (e_ != cudaSuccess) return STTM_ERR_CUDA; \
-    } while (0)
-
 inline sttm_status launched() {
     g_launches++;
     return cudaPeekAtLastError() == cudaSuccess ? STTM_OK : STTM_ERR_CUDA;
@@ -569,8 +538,6 @@ sttm_status launch_after(void (*kernel)(KArgs...), unsigned grid, unsigned block
     g_launches++;
     return e == cudaSuccess ? STTM_OK : STTM_ERR_CUDA;
 }
-
-inline unsigned blocks_for(long long items, int per_block) { return (unsigned)((items + per_block - 1) / per_block); }
 
 sttm_status run_spatial(const void* feats, const sttm_params* p, const Plan& pl, float* norms, int8_t* cover,
                         int32_t* frame_counts, float* sims, cudaStream_t st) {
@@ -798,23 +765,6 @@ sttm_status launch_pieces(const Plan& pl, int npieces, char* ws, void* out, long
 // [frame][64-channel block][y][x][64 channels] (a permutation of its dimensions in memory), so that
 // a box of NB blocks x (4x4 | 16x1 | 1x16) cells lands in shared memory block by block, each block
 // 16 rows of 128 bytes under the 128-byte swizzle.
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// the driver's tensor-map encoder, through the runtime (no link against libcuda); null when it is not there
-EncodeTiledFn tensor_map_encoder() {
-    static EncodeTiledFn encode = nullptr;
-    if (encode == nullptr) {
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) == cudaSuccess &&
-            qres == cudaDriverEntryPointSuccess)
-            encode = (EncodeTiledFn)fn;
-    }
-    return encode;
-}
-
 sttm_status make_flow_maps(const void* feats, const Geo& g, int NB, FlowMaps* maps) {
     const EncodeTiledFn encode = tensor_map_encoder();
     if (encode == nullptr) return STTM_ERR_CUDA;
@@ -1050,7 +1000,6 @@ sttm_status run_generic(const T* feats, const sttm_params* p, const Plan& pl, ch
     return launched();
 }
 
-bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
 // Scratch of sttm_spatial_static: lives in the library image, so every GPU that loads the
 // library holds these bytes until the process exits.  In host code the name below is only a

@@ -108,45 +108,9 @@ __device__ __forceinline__ const float* flow_numbers(const FlowParams& p, const 
     return p.partial + ((long long)it.item * (p.F + 1) + j) * p.NSg * kSumVals;
 }
 
-// has the phase with this parity completed?  Suspends the thread for a while (the hardware's own
-// limit) instead of returning at once: a waiting warp of these kernels must not take issue slots
-// from the warps that have work.
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-// bounded wait (see mbar_wait) on the suspending form
-__device__ __forceinline__ bool mbar_wait_sleep(uint32_t bar, int use, bool& timed_out) {
-    if (timed_out) return false;
-    const uint32_t parity = (uint32_t)(use & 1);
-    if (mbar_try(bar, parity)) return true;
-    const unsigned long long t0 = global_timer_ns();
-    while (!mbar_try(bar, parity)) {
-        if (global_timer_ns() - t0 > kWaitLimitNs) {
-            timed_out = true;
-            return false;
-        }
-    }
-    return true;
-}
 // The k-th task a kernel takes up.  The Gram stage goes through the video forwards, the sum stage
 // backwards: what the Gram stage read last is what L2 still holds when the sum stage begins.
 __device__ __forceinline__ int flow_task(bool sum_stage, int k, int ntasks) { return sum_stage ? ntasks - 1 - k : k; }
-
-// bounded wait whose outcome is the same in every lane of the warp
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, int use, bool& timed_out) {
-    const bool ok = mbar_wait_sleep(bar, use, timed_out);
-    const bool all = __all_sync(0xffffffffu, ok);
-    if (!all) timed_out = true;
-    return all;
-}
 
 // one tile of one frame, NB 64-channel blocks from block `blk0` on: global -> shared memory,
 // completion counted in bytes on an mbarrier
