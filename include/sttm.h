@@ -61,7 +61,7 @@ typedef enum {
     STTM_ERR_TIMEOUT = 7         /* a bounded wait inside a kernel ran out (device)     */
 } sttm_status;
 
-typedef enum { STTM_BF16 = 0, STTM_F32 = 1 } sttm_dtype;
+typedef enum { STTM_BF16 = 0, STTM_F32 = 1, STTM_F16 = 2 /* cache calls only */ } sttm_dtype;
 /* Section 3.4: keep the surviving token's original position, or renumber 0..N_ST-1. */
 typedef enum { STTM_POS_SURVIVED = 0, STTM_POS_REASSIGNED = 1 } sttm_pos_mode;
 /* Averaging weights inside a chain (the paper does not fix them): one per node, or the
@@ -287,6 +287,129 @@ size_t sttm_merged_positions_workspace(long long capacity_rows);
 sttm_status sttm_merged_positions(const int32_t* merge_map, const int64_t* out_offsets, int B, long long N,
                                   void* ws, size_t ws_bytes, float* out_pos_mean, long long capacity_rows,
                                   int32_t* device_status, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * The merged tokens inside a language model: a paged key-value cache of theirs.
+ *
+ * What follows the merge in a decoder layer.  sttm_cache_append takes the projections of the packed
+ * rows, with the position ids and the device-side row counts of sttm_merge_ex as they are, and fills
+ * the cache; sttm_cache_attend answers token by token; sttm_cache_evict thins a cache out by the
+ * attention its slots have received (the paper's reduction is query-agnostic: this is the step after
+ * it that knows the question).  A cache may be shared: several sequences (questions on one video) may
+ * name the same pages, since attend only reads and evict writes to other pages.
+ *
+ * A slot is one token of one sequence; slot s of sequence b lies in page table[b][s / page], at place
+ * s % page, and holds `dim` channels of keys and of values per KV head.  All types of one call are
+ * equal: bf16 or fp16 (STTM_BF16, STTM_F16).  Sums, norms and softmax statistics are fp32.
+ * ---------------------------------------------------------------------------------------------
+ */
+typedef struct sttm_cache {
+    void* k;                      /* keys of all pages                                             */
+    void* v;                      /* values, laid out like the keys                                */
+    long long pages;              /* pages behind k and v                                          */
+    int heads, page, dim;         /* KV heads; slots per page (a multiple of 8); channels: 64, 128 or 256 */
+    long long page_stride, head_stride, slot_stride;  /* in elements, multiples of 8; channels are contiguous.  Any
+                                     order of the axes will do: [pages][heads][page][dim], [pages][page][heads][dim] */
+    const int32_t* table;         /* [seqs][table_width] page of every stretch of `page` slots     */
+    long long table_stride;       /* elements from one sequence's row to the next                  */
+    int table_width;
+    int seqs;
+    sttm_dtype dtype;             /* STTM_BF16 or STTM_F16                                         */
+} sttm_cache;
+
+/*
+ * Norm, rotation and cache entry of new tokens, one pass.  Row r holds the query, key and value heads
+ * of a token; rows row_offsets[b] <= r < row_offsets[b + 1] are sequence b's, in order, and go to its
+ * slots lengths[b], lengths[b] + 1, ...  Rows at or beyond row_offsets[seqs] are not touched, so a
+ * buffer sized for all tokens of a video can be passed with the offsets that sttm_merge_ex wrote.
+ *   y = x / sqrt(mean(x^2) + eps) * w        per head of queries and keys, where w is given
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = position * inv_freq[i]
+ * for the pairs (a, b) = channels (i, i + rot / 2), or (2 i, 2 i + 1) when interleaved, i < rot / 2;
+ * channels from rot on are not rotated.  t is formed in 64 bits (fp32 would be off by 2^-24 of it, in
+ * radians, which shows from positions of some 10^5 on).  With axes = 3 a row has three positions and pair i is
+ * turned by axis 0 for i < sections[0], axis 1 for the next sections[1], axis 2 for the last sections[2]
+ * pairs (time, row and column of a token).  One rounding at the end; values are copied.
+ */
+typedef struct sttm_append_params {
+    const void *q, *k, *v;        /* [rows][q_heads | heads | heads][dim], 16-byte aligned, may be views of one tensor */
+    long long q_row, q_head, k_row, k_head, v_row, v_head;   /* strides in elements, multiples of 8 */
+    void* q_out;                  /* [rows][q_heads][dim] contiguous; may be q itself if q is so too */
+    long long rows;               /* rows behind q, k and v                                        */
+    int q_heads;                  /* 0: no queries (q and q_out NULL)                              */
+    const int64_t* row_offsets;   /* [seqs + 1]                                                    */
+    const int32_t* lengths;       /* [seqs] slots in use before the call, NULL: none               */
+    int32_t* new_lengths;         /* [seqs] out: slots in use after it, may be NULL; not `lengths` */
+    const void* positions;        /* [axes][rows] int32 or float32 (means of merged tokens)        */
+    int positions_f32;            /* nonzero: float32                                              */
+    int axes;                     /* 1 or 3                                                        */
+    long long axis_stride;        /* elements from one axis to the next (axes = 3)                 */
+    int sections[3];              /* pairs per axis (axes = 3): their sum is rot / 2               */
+    const float* inv_freq;        /* [rot / 2], any scaling included                               */
+    int rot;                      /* rotated channels: a multiple of 16, at most dim; 0: none      */
+    int interleaved;
+    const float *q_norm, *k_norm; /* [dim] weights, NULL: no norm; 16-byte aligned                 */
+    float eps;
+    int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_CAPACITY (a slot beyond the table: its
+                                     key and value are dropped) and 1 << STTM_ERR_ARG (a page that is not there: dropped) */
+} sttm_append_params;
+sttm_status sttm_cache_append(const sttm_cache* cache, const sttm_append_params* p, void* stream);
+
+/*
+ * Attention of one new token per sequence over its cache.
+ *   out[b, h] = sum over slots s of p[h, s] v[s, h / group],  p[h, s] = softmax over s of scale q[b, h] . k[s, h / group]
+ * with group = q_heads / heads, over the slots s < lengths[b] whose mask byte (if there is a mask) is not
+ * zero.  What lies in other slots (rubbish, NaN) does not matter.  A sequence with no such slot gives
+ * out = 0 and lse = -inf.  An infinite value in a slot that does count gives inf or NaN.
+ *   scores[b, h, s] = decay * scores[b, h, s] + sum of p over the query heads of KV head h
+ * for s < lengths[b] (with a zero mask byte: decay alone), where scores are wanted.
+ */
+typedef struct sttm_attend_params {
+    const void* q;                /* [seqs][q_heads][dim], 16-byte aligned                         */
+    long long q_seq, q_head;      /* strides in elements, multiples of 8                           */
+    int q_heads;                  /* a multiple of the cache's heads, at most 64 per KV head       */
+    const int32_t* lengths;       /* [seqs] slots in use (the new token's own among them)          */
+    int max_len;                  /* no length is larger (else it is cut and 1 << STTM_ERR_CAPACITY raised); at most
+                                     table_width * page */
+    float scale;
+    const uint8_t* mask;          /* [seqs][mask_stride], mask_stride >= max_len, or NULL          */
+    long long mask_stride;
+    float* scores;                /* in and out, or NULL                                           */
+    long long score_seq, score_head;   /* strides in elements, from one sequence / KV head to the next */
+    float decay;
+    void* out;                    /* [seqs][q_heads][dim] contiguous                               */
+    float* lse;                   /* [seqs][q_heads] log of the sum of exp(scale q . k), may be NULL */
+    int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_CAPACITY, 1 << STTM_ERR_ARG (a page that is
+                                     not there: read as zeros), 1 << STTM_ERR_TIMEOUT */
+} sttm_attend_params;
+/* Workspace of a call: depends on seqs, heads, dim, q_heads, max_len and on whether scores are wanted; any
+ * contents; 256-byte aligned.  0 on bad params. */
+size_t sttm_attend_workspace_bytes(const sttm_cache* cache, const sttm_attend_params* p);
+sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params* p, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/*
+ * Keeps, of every sequence and KV head, the keep[b] slots with the highest scores, in their order, and
+ * copies their keys and values to slots 0, 1, ... of the same sequence in `dst`, whose pages are other pages
+ * than src's (of the same pool or of another; both caches have the same heads, dim, dtype and seqs).
+ * The first `first` and the last `last` slots of a sequence come before all others; equal scores: the
+ * lowest slot first; NaN after every number.  What is kept is also limited by kept_width and by dst's table
+ * (1 << STTM_ERR_CAPACITY where that cuts).
+ */
+typedef struct sttm_evict_params {
+    const int32_t* lengths;       /* [seqs] slots in use                                           */
+    int max_len;                  /* as for sttm_cache_attend                                      */
+    const int32_t* keep;          /* [seqs] slots to keep                                          */
+    int first, last;              /* protected slots                                               */
+    const float* scores;          /* [seqs][heads][max_len]                                        */
+    long long score_seq, score_head;   /* strides in elements                                      */
+    int kept_width;               /* columns of kept and new_scores                                */
+    int32_t* new_lengths;         /* [seqs] out                                                    */
+    int32_t* kept;                /* [seqs][heads][kept_width] out: the slots kept, then -1        */
+    float* new_scores;            /* [seqs][heads][kept_width] out: their scores, then 0           */
+    int32_t* device_status;       /* may be NULL; also 1 << STTM_ERR_ARG (a page that is not there: not copied) */
+} sttm_evict_params;
+sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const sttm_evict_params* p, void* stream);
 
 /* Frees the cached buffers of sttm_merge / sttm_merge_host on the current device. */
 void sttm_release_cache(void);

@@ -1,0 +1,300 @@
+"""The merged tokens inside a language model: a paged key-value cache of theirs.
+
+``AppendPlan`` (norm of queries and keys, rotation by position ids, cache entry), ``AttendPlan``
+(attention of one new token per sequence) and ``EvictPlan`` (keeps the slots that received most
+attention) marshal arguments for sttm_cache_append, sttm_cache_attend and sttm_cache_evict; a plan
+holds buffers and parameters for repeated calls on one cache.  The functions of those names are
+single calls.  All work is enqueued on the current stream, nothing synchronises; conditions found
+on the device are OR-ed into a plan's ``status``, which it never clears.  There is no fallback.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+from dataclasses import dataclass
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding
+from .binding import _check, _stream
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 2}
+
+
+class SttmCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_longlong), ("heads", C.c_int), ("page", C.c_int),
+                ("dim", C.c_int), ("page_stride", C.c_longlong), ("head_stride", C.c_longlong),
+                ("slot_stride", C.c_longlong), ("table", C.c_void_p), ("table_stride", C.c_longlong),
+                ("table_width", C.c_int), ("seqs", C.c_int), ("dtype", C.c_int)]
+
+
+class AppendParams(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_row", C.c_longlong), ("q_head", C.c_longlong),
+                ("k_row", C.c_longlong), ("k_head", C.c_longlong), ("v_row", C.c_longlong), ("v_head", C.c_longlong),
+                ("q_out", C.c_void_p), ("rows", C.c_longlong), ("q_heads", C.c_int), ("row_offsets", C.c_void_p),
+                ("lengths", C.c_void_p), ("new_lengths", C.c_void_p), ("positions", C.c_void_p), ("positions_f32", C.c_int),
+                ("axes", C.c_int), ("axis_stride", C.c_longlong), ("sections", C.c_int * 3), ("inv_freq", C.c_void_p),
+                ("rot", C.c_int), ("interleaved", C.c_int), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p),
+                ("eps", C.c_float), ("device_status", C.c_void_p)]
+
+
+class AttendParams(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_seq", C.c_longlong), ("q_head", C.c_longlong), ("q_heads", C.c_int),
+                ("lengths", C.c_void_p), ("max_len", C.c_int), ("scale", C.c_float), ("mask", C.c_void_p),
+                ("mask_stride", C.c_longlong), ("scores", C.c_void_p), ("score_seq", C.c_longlong),
+                ("score_head", C.c_longlong), ("decay", C.c_float), ("out", C.c_void_p), ("lse", C.c_void_p),
+                ("device_status", C.c_void_p)]
+
+
+class EvictParams(C.Structure):
+    _fields_ = [("lengths", C.c_void_p), ("max_len", C.c_int), ("keep", C.c_void_p), ("first", C.c_int), ("last", C.c_int),
+                ("scores", C.c_void_p), ("score_seq", C.c_longlong), ("score_head", C.c_longlong), ("kept_width", C.c_int),
+                ("new_lengths", C.c_void_p), ("kept", C.c_void_p), ("new_scores", C.c_void_p), ("device_status", C.c_void_p)]
+
+
+def _want(ok: bool, text: str) -> None:
+    if not ok:
+        raise ValueError(text)
+
+
+def _ints(t: torch.Tensor, n: int, what: str, device) -> int:
+    _want(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.device == device,
+          "%s must be a contiguous int32 tensor [%d] on the cache's device" % (what, n))
+    return t.data_ptr()
+
+
+class PagedCache:
+    """Pools of keys and values and a page table.  ``k`` and ``v``: ``[pages, heads, page, dim]`` bf16 or
+    fp16 CUDA tensors with contiguous channels (a pool laid out slot by slot is passed as
+    ``pool.transpose(1, 2)``); ``table``: int32 ``[seqs, width]``, the page of every stretch of ``page`` slots."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+        _want(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.dtype in _DTYPES
+              and k.is_cuda and v.device == k.device and k.stride(3) == 1,
+              "k and v must be bf16 or fp16 CUDA tensors [pages, heads, page, dim], alike, with contiguous channels")
+        _want(table.dim() == 2 and table.dtype == torch.int32 and table.device == k.device and table.stride(1) == 1,
+              "table must be an int32 CUDA tensor [seqs, width] with contiguous rows")
+        self.k, self.v, self.table, self.device, self.dtype = k, v, table, k.device, k.dtype
+        self.pages, self.heads, self.page, self.dim = k.shape
+        self.seqs, self.width = table.shape
+        self.struct = SttmCache(k.data_ptr(), v.data_ptr(), self.pages, self.heads, self.page, self.dim, k.stride(0),
+                                k.stride(1), k.stride(2), table.data_ptr(), table.stride(0), self.width, self.seqs,
+                                _DTYPES[k.dtype])
+
+    def on_current_device(self) -> None:
+        _want(self.device.index == torch.cuda.current_device(), "the cache is not on the current CUDA device")
+
+
+def empty_cache(seqs: int, max_len: int, heads: int, dim: int, page: int = 64, dtype: torch.dtype = torch.bfloat16,
+                device="cuda") -> PagedCache:
+    """A cache with pages of its own for ``max_len`` slots of every sequence."""
+    width = -(-max_len // page)
+    k, v = (torch.empty((seqs * width, heads, page, dim), dtype=dtype, device=device) for _ in range(2))
+    return PagedCache(k, v, torch.arange(seqs * width, dtype=torch.int32, device=k.device).view(seqs, width))
+
+
+@dataclass
+class Rotary:
+    """Rotation by position: ``inv_freq`` float32 ``[rot / 2]`` on the device.  Pairs are channels (i, i + rot / 2), or
+    (2 i, 2 i + 1) when ``interleaved``.  ``sections``: pairs turned by each of three positions (time, row, column)."""
+    inv_freq: torch.Tensor
+    interleaved: bool = False
+    sections: Optional[Sequence[int]] = None
+
+
+@dataclass
+class AppendOutput:
+    q: Optional[torch.Tensor]        # [rows, q_heads, dim]: queries, normed and rotated
+    new_lengths: torch.Tensor        # [seqs] int32
+    status: torch.Tensor
+
+
+class AppendPlan:
+    """Repeated sttm_cache_append calls on one cache."""
+
+    def __init__(self, cache: PagedCache, q_heads: int, rotary: Optional[Rotary] = None, q_norm: Optional[torch.Tensor] = None,
+                 k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        self.cache, self.q_heads, self.rotary, self.keep = cache, q_heads, rotary, (q_norm, k_norm)
+        self.new_lengths = torch.zeros((2, cache.seqs), dtype=torch.int32, device=cache.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        p = self.params = AppendParams()
+        p.q_heads, p.eps, p.axes = q_heads, eps, 1
+        p.device_status = self.status.data_ptr()
+        if rotary is not None:
+            f = rotary.inv_freq
+            _want(f.dtype == torch.float32 and f.dim() == 1 and f.is_contiguous() and f.device == cache.device,
+                  "inv_freq must be a contiguous float32 tensor [rot / 2] on the cache's device")
+            p.inv_freq, p.rot, p.interleaved = f.data_ptr(), 2 * f.shape[0], int(rotary.interleaved)
+            if rotary.sections is not None:
+                _want(len(rotary.sections) == 3, "sections must be three numbers")
+                p.axes = 3
+                p.sections[:] = [int(x) for x in rotary.sections]
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None:
+                _want(w.dtype == torch.float32 and tuple(w.shape) == (cache.dim,) and w.is_contiguous() and w.device == cache.device,
+                      "%s must be a contiguous float32 tensor [dim] on the cache's device" % name)
+                setattr(p, name, w.data_ptr())
+
+    def run(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, row_offsets: torch.Tensor,
+            lengths: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+            q_out: Optional[torch.Tensor] = None) -> AppendOutput:
+        """``q`` ``[rows, q_heads, dim]``, ``k``, ``v`` ``[rows, heads, dim]`` (any row and head strides, views of one
+        projection for instance); ``row_offsets`` int64 ``[seqs + 1]``; ``lengths`` int32 ``[seqs]`` (None: an empty cache);
+        ``positions`` int32 or float32 ``[rows]`` or ``[axes, rows]``.  ``new_lengths`` of the result is valid until
+        the call after the next."""
+        c, p = self.cache, self.params
+        c.on_current_device()
+        rows = k.shape[0]
+        for name, t, heads in (("q", q, self.q_heads), ("k", k, c.heads), ("v", v, c.heads)):
+            if t is None:
+                _want(name == "q" and heads == 0, "%s is missing" % name)
+                continue
+            _want(t.shape == (rows, heads, c.dim) and t.dtype == c.dtype and t.device == c.device and (rows == 0 or t.stride(2) == 1),
+                  "%s must be [rows, %d, %d] of the cache's type, on its device, with contiguous channels" % (name, heads, c.dim))
+            s = t.stride()
+            setattr(p, name, t.data_ptr())
+            setattr(p, name + "_row", s[0] if rows > 1 else 0)
+            setattr(p, name + "_head", s[1] if heads > 1 else 0)
+        _want(row_offsets.dtype == torch.int64 and row_offsets.shape == (c.seqs + 1,) and row_offsets.is_contiguous()
+              and row_offsets.device == c.device, "row_offsets must be a contiguous int64 tensor [seqs + 1] on the cache's device")
+        p.row_offsets, p.rows = row_offsets.data_ptr(), rows
+        p.lengths = None if lengths is None else _ints(lengths, c.seqs, "lengths", c.device)
+        new = self.new_lengths[0] if p.lengths != self.new_lengths.data_ptr() else self.new_lengths[1]
+        p.new_lengths = new.data_ptr()
+        if p.rot > 0:
+            _want(positions is not None and positions.dtype in (torch.int32, torch.float32) and positions.device == c.device
+                  and positions.numel() == p.axes * rows and positions.shape[-1] == rows and (rows < 2 or positions.stride(-1) == 1),
+                  "positions must be int32 or float32 [axes, rows] on the cache's device")
+            p.positions, p.positions_f32 = positions.data_ptr(), int(positions.dtype == torch.float32)
+            p.axis_stride = positions.stride(0) if p.axes == 3 else 0
+        if self.q_heads > 0 and q_out is None:
+            q_out = torch.empty((rows, self.q_heads, c.dim), dtype=c.dtype, device=c.device)
+        if q_out is not None:
+            _want(q_out.shape == (rows, self.q_heads, c.dim) and q_out.dtype == c.dtype and q_out.is_contiguous() and q_out.device == c.device,
+                  "q_out must be contiguous [rows, q_heads, dim] of the cache's type")
+            p.q_out = q_out.data_ptr()
+        _check(binding.load_library().sttm_cache_append(C.byref(c.struct), C.byref(p), _stream()), "sttm_cache_append")
+        return AppendOutput(q_out, new, self.status)
+
+
+@dataclass
+class AttendOutput:
+    out: torch.Tensor                # [seqs, q_heads, dim]
+    lse: torch.Tensor                # [seqs, q_heads] float32: log of the sum of the exponentials
+    status: torch.Tensor
+
+
+class AttendPlan:
+    """Repeated sttm_cache_attend calls on one cache; ``out`` and ``lse`` are the plan's own buffers."""
+
+    def __init__(self, cache: PagedCache, q_heads: int, scale: Optional[float] = None, max_len: Optional[int] = None,
+                 decay: float = 1.0):
+        self.cache, self.q_heads = cache, q_heads
+        self.max_len = cache.width * cache.page if max_len is None else int(max_len)
+        self.out = torch.empty((cache.seqs, q_heads, cache.dim), dtype=cache.dtype, device=cache.device)
+        self.lse = torch.empty((cache.seqs, q_heads), dtype=torch.float32, device=cache.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        p = self.params = AttendParams()
+        p.q_heads, p.max_len, p.decay = q_heads, self.max_len, decay
+        p.scale = 1.0 / math.sqrt(cache.dim) if scale is None else scale
+        p.out, p.lse, p.device_status = self.out.data_ptr(), self.lse.data_ptr(), self.status.data_ptr()
+        self.ws = {}
+
+    def _workspace(self, scored: bool) -> torch.Tensor:
+        ws = self.ws.get(scored)
+        if ws is None:
+            n = int(binding.load_library().sttm_attend_workspace_bytes(C.byref(self.cache.struct), C.byref(self.params)))
+            # (0: the call itself names the reason)
+            ws = self.ws[scored] = torch.empty(max(n, 256), dtype=torch.uint8, device=self.cache.device)
+        return ws
+
+    def run(self, q: torch.Tensor, lengths: torch.Tensor, mask: Optional[torch.Tensor] = None,
+            scores: Optional[torch.Tensor] = None) -> AttendOutput:
+        """``q`` ``[seqs, q_heads, dim]``; ``lengths`` int32 ``[seqs]``; ``mask`` bool or uint8 ``[seqs, >= max_len]``,
+        false: slot left out; ``scores`` float32 ``[seqs, heads, >= max_len]``, updated in place."""
+        c, p = self.cache, self.params
+        c.on_current_device()
+        _want(q.shape == (c.seqs, self.q_heads, c.dim) and q.dtype == c.dtype and q.device == c.device and q.stride(2) == 1,
+              "q must be [seqs, q_heads, dim] of the cache's type, on its device, with contiguous channels")
+        s = q.stride()
+        p.q, p.q_seq, p.q_head = q.data_ptr(), s[0] if c.seqs > 1 else 0, s[1] if self.q_heads > 1 else 0
+        p.lengths = _ints(lengths, c.seqs, "lengths", c.device)
+        if mask is None:
+            p.mask = None
+        else:
+            _want(mask.dim() == 2 and mask.shape[0] == c.seqs and mask.shape[1] >= self.max_len and mask.dtype in (torch.bool, torch.uint8)
+                  and mask.stride(1) == 1 and mask.device == c.device, "mask must be bool or uint8 [seqs, >= max_len] with contiguous rows")
+            p.mask, p.mask_stride = mask.data_ptr(), mask.stride(0)
+        if scores is None:
+            p.scores = None
+        else:
+            _want_scores(scores, c, self.max_len)
+            p.scores, p.score_seq, p.score_head = scores.data_ptr(), scores.stride(0), scores.stride(1)
+        ws = self._workspace(scores is not None)
+        _check(binding.load_library().sttm_cache_attend(C.byref(c.struct), C.byref(p), ws.data_ptr(), ws.numel(), _stream()),
+               "sttm_cache_attend")
+        return AttendOutput(self.out, self.lse, self.status)
+
+
+def _want_scores(scores: torch.Tensor, c: PagedCache, max_len: int) -> None:
+    _want(scores.dim() == 3 and scores.shape[0] == c.seqs and scores.shape[1] == c.heads and scores.shape[2] >= max_len
+          and scores.dtype == torch.float32 and scores.stride(2) == 1 and scores.device == c.device,
+          "scores must be float32 [seqs, heads, >= max_len] with contiguous slots, on the cache's device")
+
+
+@dataclass
+class EvictOutput:
+    new_lengths: torch.Tensor        # [seqs] int32
+    kept: torch.Tensor               # [seqs, heads, kept_width] int32: slots of the source, then -1
+    new_scores: torch.Tensor         # [seqs, heads, kept_width] float32: their scores, then 0
+    status: torch.Tensor
+
+
+class EvictPlan:
+    """Repeated sttm_cache_evict calls from one cache to another (pages of its own); outputs are the plan's buffers."""
+
+    def __init__(self, src: PagedCache, dst: PagedCache, kept_width: int, first: int = 0, last: int = 0,
+                 max_len: Optional[int] = None):
+        _want(dst.device == src.device, "both caches must be on one device")
+        self.src, self.dst = src, dst
+        self.max_len = src.width * src.page if max_len is None else int(max_len)
+        shape = (src.seqs, src.heads, kept_width)
+        self.new_lengths = torch.zeros(src.seqs, dtype=torch.int32, device=src.device)
+        self.kept = torch.empty(shape, dtype=torch.int32, device=src.device)
+        self.new_scores = torch.empty(shape, dtype=torch.float32, device=src.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=src.device)
+        p = self.params = EvictParams()
+        p.max_len, p.first, p.last, p.kept_width = self.max_len, first, last, kept_width
+        p.new_lengths, p.kept, p.new_scores = self.new_lengths.data_ptr(), self.kept.data_ptr(), self.new_scores.data_ptr()
+        p.device_status = self.status.data_ptr()
+
+    def run(self, lengths: torch.Tensor, keep: torch.Tensor, scores: torch.Tensor) -> EvictOutput:
+        """``lengths``, ``keep`` int32 ``[seqs]``; ``scores`` float32 ``[seqs, heads, >= max_len]``."""
+        c, p = self.src, self.params
+        c.on_current_device()
+        p.lengths = _ints(lengths, c.seqs, "lengths", c.device)
+        p.keep = _ints(keep, c.seqs, "keep", c.device)
+        _want_scores(scores, c, self.max_len)
+        p.scores, p.score_seq, p.score_head = scores.data_ptr(), scores.stride(0), scores.stride(1)
+        _check(binding.load_library().sttm_cache_evict(C.byref(c.struct), C.byref(self.dst.struct), C.byref(p), _stream()),
+               "sttm_cache_evict")
+        return EvictOutput(self.new_lengths, self.kept, self.new_scores, self.status)
+
+
+def sttm_cache_append(cache: PagedCache, q, k, v, row_offsets, lengths=None, positions=None, rotary: Optional[Rotary] = None,
+                      q_norm=None, k_norm=None, eps: float = 1e-6) -> AppendOutput:
+    """Norm, rotation and cache entry of new tokens; see AppendPlan.run."""
+    return AppendPlan(cache, 0 if q is None else q.shape[1], rotary, q_norm, k_norm, eps).run(q, k, v, row_offsets, lengths, positions)
+
+
+def sttm_cache_attend(cache: PagedCache, q, lengths, mask=None, scores=None, scale: Optional[float] = None,
+                      max_len: Optional[int] = None, decay: float = 1.0) -> AttendOutput:
+    """Attention of one new token per sequence; see AttendPlan.run."""
+    return AttendPlan(cache, q.shape[1], scale, max_len, decay).run(q, lengths, mask, scores)
+
+
+def sttm_cache_evict(src: PagedCache, dst: PagedCache, lengths, keep, scores, kept_width: int, first: int = 0, last: int = 0,
+                     max_len: Optional[int] = None) -> EvictOutput:
+    """Keeps the highest-scored slots; see EvictPlan.run."""
+    return EvictPlan(src, dst, kept_width, first, last, max_len).run(lengths, keep, scores)

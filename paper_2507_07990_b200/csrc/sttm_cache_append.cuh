@@ -1,0 +1,161 @@
+// Norm, rotation and cache entry of new tokens (sttm_cache_append).
+//
+// Every channel is read once and written once; the arithmetic in between (a sum of squares, a
+// product, a turn) is a few operations per channel, so HBM bounds the kernel.  A head is taken by
+// DIM / 16 lanes, two 16-byte words each, chosen so that both channels of every rotated pair lie in
+// one lane: words c and c + rot / 16 for pairs (i, i + rot / 2), words 2 c and 2 c + 1 for pairs
+// (2 i, 2 i + 1).  Either way lane c needs the angles 8 c ... 8 c + 7, the same for every head: the
+// warp forms the row's rot / 2 angles once, two or so per lane, and passes them round through shared
+// memory.
+#pragma once
+
+#include "sttm_cache.cuh"
+
+namespace sttm {
+
+struct AppendArgs {
+    CacheView c;
+    const uint16_t *q, *k, *v;
+    long long q_row, q_head, k_row, k_head, v_row, v_head;
+    uint16_t* q_out;
+    long long rows;
+    int q_heads;
+    const long long* row_offsets;
+    const int32_t* lengths;
+    int32_t* new_lengths;
+    const void* positions;
+    int positions_f32;
+    long long axis_stride;
+    int sec0, sec1;               // pairs below sec0 turn by axis 0, below sec1 by axis 1, the others by axis 2
+    const float* inv_freq;
+    int rot;
+    const float *q_norm, *k_norm;
+    float eps;
+    int32_t* status;
+    int parts;                    // warps that share one row's heads
+};
+
+constexpr int kAppendWarps = 4;
+
+// sequence of a row: the number of offsets [1 .. seqs] that are <= row, found by the whole warp, 32 probes a step
+__device__ __forceinline__ int sequence_of(const long long* offsets, int seqs, long long row, int lane) {
+    int lo = 0, n = seqs;                                   // answer in [lo, lo + n]
+    while (n > 0) {
+        const int step = (n + 31) / 32;                     // probe offsets lo + step, lo + 2 step, ...
+        const int at = lo + (lane + 1) * step;
+        const bool below = at <= lo + n && offsets[at] <= row;
+        const int hits = __popc(__ballot_sync(0xffffffffu, below));
+        lo += hits * step;
+        n = min(step - 1, n - hits * step);
+    }
+    return min(lo, seqs - 1);
+}
+
+template <typename T, int DIM, bool INTERLEAVED>
+__global__ void __launch_bounds__(kAppendWarps * 32) k_cache_append(const __grid_constant__ AppendArgs a) {
+    constexpr int LPH = DIM / 16;                           // lanes per head
+    constexpr int HPW = 32 / LPH;                           // heads per warp and step
+    __shared__ float2 turns[kAppendWarps][DIM / 2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    wait_for_prior_kernel();
+    let_next_kernel_start();
+    const int seqs = a.c.seqs;
+    if (a.new_lengths != nullptr && blockIdx.x == 0)
+        for (int b = threadIdx.x; b < seqs; b += blockDim.x)
+            a.new_lengths[b] = (a.lengths ? a.lengths[b] : 0) + (int)(a.row_offsets[b + 1] - a.row_offsets[b]);
+    const long long w = (long long)blockIdx.x * kAppendWarps + warp;
+    const long long row = w / a.parts;
+    const int part = (int)(w - row * a.parts);
+    if (row >= a.rows || row >= a.row_offsets[seqs]) return;
+    const int seq = sequence_of(a.row_offsets, seqs, row, lane);
+    const long long slot = (a.lengths ? a.lengths[seq] : 0) + (row - a.row_offsets[seq]);
+    const long long at = slot_at(a.c, seq, slot, lane == 0 && part == 0 ? a.status : nullptr);
+
+    // the row's turns.  The angle in turns is formed in 64 bits and brought into [-1/2, 1/2] there.
+    for (int i = lane; i < a.rot / 2; i += 32) {
+        const long long pi = row + (i < a.sec0 ? 0 : (i < a.sec1 ? a.axis_stride : 2 * a.axis_stride));
+        const double pos = a.positions_f32 ? (double)((const float*)a.positions)[pi] : (double)((const int32_t*)a.positions)[pi];
+        const double t = pos * (double)a.inv_freq[i] * 0.15915494309189533577;     // 1 / (2 pi)
+        float s, c;
+        sincospif(2.f * (float)(t - rint(t)), &s, &c);
+        turns[warp][i] = make_float2(c, s);
+    }
+    __syncwarp();
+
+    const int c = lane % LPH, sub = lane / LPH;
+    const int rw = a.rot / 16;                              // rotated words per half = lanes that turn
+    int w0, w1;                                             // this lane's 16-byte words of a head
+    if (INTERLEAVED) { w0 = 2 * c; w1 = 2 * c + 1; }
+    else if (c < rw) { w0 = c; w1 = c + rw; }
+    else { w0 = 2 * c; w1 = 2 * c + 1; }                    // (channels from rot on: words 2 rw + 2 (c - rw), and the next)
+    const bool turn = c < rw;
+    float2 cs[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) cs[e] = turn ? turns[warp][8 * c + e] : make_float2(1.f, 0.f);
+
+    const int heads = a.q_heads + 2 * a.c.heads;
+    for (int h0 = part * HPW; h0 < heads; h0 += a.parts * HPW) {
+        const int h = h0 + sub;
+        const bool mine = h < heads;
+        const int kind = h < a.q_heads ? 0 : (h < a.q_heads + a.c.heads ? 1 : 2);
+        const int hh = h - (kind == 0 ? 0 : (kind == 1 ? a.q_heads : a.q_heads + a.c.heads));
+        const uint16_t* src = kind == 0 ? a.q + row * a.q_row + hh * a.q_head
+                                        : (kind == 1 ? a.k + row * a.k_row + hh * a.k_head : a.v + row * a.v_row + hh * a.v_head);
+        uint16_t* dst = kind == 0 ? a.q_out + (row * a.q_heads + hh) * DIM
+                                  : (at < 0 ? nullptr : (kind == 1 ? a.c.k : a.c.v) + at + hh * a.c.head_stride);
+        uint4 x0 = {}, x1 = {};
+        if (mine) {
+            x0 = reinterpret_cast<const uint4*>(src)[w0];
+            x1 = reinterpret_cast<const uint4*>(src)[w1];
+        }
+        float f[16];
+        {
+            const uint32_t u[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float2 p = Pair<T>::split(u[e]);
+                f[2 * e] = p.x;
+                f[2 * e + 1] = p.y;
+            }
+        }
+        const float* wt = kind == 0 ? a.q_norm : (kind == 1 ? a.k_norm : nullptr);
+        if (a.q_norm != nullptr || a.k_norm != nullptr) {   // (the same for the whole warp: the lanes of a head add up their squares)
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; e++) ss = fmaf(f[e], f[e], ss);
+#pragma unroll
+            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            if (wt != nullptr) {
+                const float r = 1.f / sqrtf(ss * (1.f / DIM) + a.eps);
+                const float4* w4 = reinterpret_cast<const float4*>(wt);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float4 g = __ldg(w4 + (e < 2 ? 2 * w0 + e : 2 * w1 + e - 2));
+                    f[4 * e] = f[4 * e] * r * g.x;
+                    f[4 * e + 1] = f[4 * e + 1] * r * g.y;
+                    f[4 * e + 2] = f[4 * e + 2] * r * g.z;
+                    f[4 * e + 3] = f[4 * e + 3] * r * g.w;
+                }
+            }
+        }
+        if (kind != 2) {
+            if (turn) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    float &p = INTERLEAVED ? f[2 * e] : f[e], &s = INTERLEAVED ? f[2 * e + 1] : f[e + 8];
+                    const float y = p * cs[e].x - s * cs[e].y;
+                    s = s * cs[e].x + p * cs[e].y;
+                    p = y;
+                }
+            }
+            x0 = make_uint4(Pair<T>::pack(f[0], f[1]), Pair<T>::pack(f[2], f[3]), Pair<T>::pack(f[4], f[5]), Pair<T>::pack(f[6], f[7]));
+            x1 = make_uint4(Pair<T>::pack(f[8], f[9]), Pair<T>::pack(f[10], f[11]), Pair<T>::pack(f[12], f[13]), Pair<T>::pack(f[14], f[15]));
+        }
+        if (mine && dst != nullptr) {
+            reinterpret_cast<uint4*>(dst)[w0] = x0;
+            reinterpret_cast<uint4*>(dst)[w1] = x1;
+        }
+    }
+}
+
+}  // namespace sttm
