@@ -17,7 +17,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import binding
-from .binding import _check, _stream
+from .binding import _check
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 2}
 
@@ -58,10 +58,25 @@ def _want(ok: bool, text: str) -> None:
         raise ValueError(text)
 
 
-def _ints(t: torch.Tensor, n: int, what: str, device) -> int:
-    _want(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.device == device,
-          "%s must be a contiguous int32 tensor [%d] on the cache's device" % (what, n))
+def _fits(t: torch.Tensor, shape: tuple, dtype: torch.dtype, index: int) -> bool:
+    return t.dtype is dtype and t.shape == shape and t.get_device() == index
+
+
+def _ints(t: torch.Tensor, shape: tuple, what: str, index: int) -> int:
+    if not (_fits(t, shape, torch.int32, index) and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous int32 tensor [%d] on the cache's device" % (what, shape[0]))
     return t.data_ptr()
+
+
+def _heads(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, index: int, what: str):
+    """Address, row stride and head stride of [rows, heads, dim] (any strides of the first two axes)."""
+    if t is None or not _fits(t, shape, dtype, index):
+        raise ValueError("%s must be a %s tensor %s on the cache's device" % (what, dtype, list(shape)))
+    row, head, channel = t.stride()
+    if channel != 1 and shape[0] > 0:
+        raise ValueError("%s must have contiguous channels" % what)
+    # (the stride of an axis of length one says nothing)
+    return t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
 
 
 class PagedCache:
@@ -76,14 +91,20 @@ class PagedCache:
         _want(table.dim() == 2 and table.dtype == torch.int32 and table.device == k.device and table.stride(1) == 1,
               "table must be an int32 CUDA tensor [seqs, width] with contiguous rows")
         self.k, self.v, self.table, self.device, self.dtype = k, v, table, k.device, k.dtype
+        self.index = k.get_device()
         self.pages, self.heads, self.page, self.dim = k.shape
         self.seqs, self.width = table.shape
         self.struct = SttmCache(k.data_ptr(), v.data_ptr(), self.pages, self.heads, self.page, self.dim, k.stride(0),
                                 k.stride(1), k.stride(2), table.data_ptr(), table.stride(0), self.width, self.seqs,
                                 _DTYPES[k.dtype])
+        self.at = C.byref(self.struct)
 
-    def on_current_device(self) -> None:
-        _want(self.device.index == torch.cuda.current_device(), "the cache is not on the current CUDA device")
+    def stream(self) -> int:
+        """The current stream of the cache's device, which has to be the current device."""
+        if torch._C._cuda_getDevice() != self.index:
+            raise ValueError("the cache is not on the current CUDA device")
+        # the handle alone: torch.cuda.current_stream() makes a stream object, which takes as long as a small call
+        return torch._C._cuda_getCurrentRawStream(self.index)
 
 
 def empty_cache(seqs: int, max_len: int, heads: int, dim: int, page: int = 64, dtype: torch.dtype = torch.bfloat16,
@@ -116,9 +137,12 @@ class AppendPlan:
     def __init__(self, cache: PagedCache, q_heads: int, rotary: Optional[Rotary] = None, q_norm: Optional[torch.Tensor] = None,
                  k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
         self.cache, self.q_heads, self.rotary, self.keep = cache, q_heads, rotary, (q_norm, k_norm)
-        self.new_lengths = torch.zeros((2, cache.seqs), dtype=torch.int32, device=cache.device)
+        # two of them: the lengths that a call reads may be those that the call before it wrote
+        self.new_lengths = [torch.zeros(cache.seqs, dtype=torch.int32, device=cache.device) for _ in range(2)]
+        self.new_at = [t.data_ptr() for t in self.new_lengths]
         self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
         p = self.params = AppendParams()
+        self.at, self.call = C.byref(p), binding.load_library().sttm_cache_append
         p.q_heads, p.eps, p.axes = q_heads, eps, 1
         p.device_status = self.status.data_ptr()
         if rotary is not None:
@@ -144,37 +168,31 @@ class AppendPlan:
         ``positions`` int32 or float32 ``[rows]`` or ``[axes, rows]``.  ``new_lengths`` of the result is valid until
         the call after the next."""
         c, p = self.cache, self.params
-        c.on_current_device()
-        rows = k.shape[0]
-        for name, t, heads in (("q", q, self.q_heads), ("k", k, c.heads), ("v", v, c.heads)):
-            if t is None:
-                _want(name == "q" and heads == 0, "%s is missing" % name)
-                continue
-            _want(t.shape == (rows, heads, c.dim) and t.dtype == c.dtype and t.device == c.device and (rows == 0 or t.stride(2) == 1),
-                  "%s must be [rows, %d, %d] of the cache's type, on its device, with contiguous channels" % (name, heads, c.dim))
-            s = t.stride()
-            setattr(p, name, t.data_ptr())
-            setattr(p, name + "_row", s[0] if rows > 1 else 0)
-            setattr(p, name + "_head", s[1] if heads > 1 else 0)
-        _want(row_offsets.dtype == torch.int64 and row_offsets.shape == (c.seqs + 1,) and row_offsets.is_contiguous()
-              and row_offsets.device == c.device, "row_offsets must be a contiguous int64 tensor [seqs + 1] on the cache's device")
-        p.row_offsets, p.rows = row_offsets.data_ptr(), rows
-        p.lengths = None if lengths is None else _ints(lengths, c.seqs, "lengths", c.device)
-        new = self.new_lengths[0] if p.lengths != self.new_lengths.data_ptr() else self.new_lengths[1]
-        p.new_lengths = new.data_ptr()
-        if p.rot > 0:
-            _want(positions is not None and positions.dtype in (torch.int32, torch.float32) and positions.device == c.device
-                  and positions.numel() == p.axes * rows and positions.shape[-1] == rows and (rows < 2 or positions.stride(-1) == 1),
-                  "positions must be int32 or float32 [axes, rows] on the cache's device")
-            p.positions, p.positions_f32 = positions.data_ptr(), int(positions.dtype == torch.float32)
-            p.axis_stride = positions.stride(0) if p.axes == 3 else 0
-        if self.q_heads > 0 and q_out is None:
-            q_out = torch.empty((rows, self.q_heads, c.dim), dtype=c.dtype, device=c.device)
-        if q_out is not None:
-            _want(q_out.shape == (rows, self.q_heads, c.dim) and q_out.dtype == c.dtype and q_out.is_contiguous() and q_out.device == c.device,
-                  "q_out must be contiguous [rows, q_heads, dim] of the cache's type")
+        dim, dtype, index, rows = c.dim, c.dtype, c.index, k.shape[0]
+        if self.q_heads > 0:
+            p.q, p.q_row, p.q_head = _heads(q, (rows, self.q_heads, dim), dtype, index, "q")
+            if q_out is None:
+                q_out = torch.empty((rows, self.q_heads, dim), dtype=dtype, device=c.device)
+            elif not (_fits(q_out, (rows, self.q_heads, dim), dtype, index) and q_out.is_contiguous()):
+                raise ValueError("q_out must be contiguous [rows, q_heads, dim] of the cache's type")
             p.q_out = q_out.data_ptr()
-        _check(binding.load_library().sttm_cache_append(C.byref(c.struct), C.byref(p), _stream()), "sttm_cache_append")
+        p.k, p.k_row, p.k_head = _heads(k, (rows, c.heads, dim), dtype, index, "k")
+        p.v, p.v_row, p.v_head = _heads(v, (rows, c.heads, dim), dtype, index, "v")
+        if not (_fits(row_offsets, (c.seqs + 1,), torch.int64, index) and row_offsets.is_contiguous()):
+            raise ValueError("row_offsets must be a contiguous int64 tensor [seqs + 1] on the cache's device")
+        p.row_offsets, p.rows = row_offsets.data_ptr(), rows
+        p.lengths = at = None if lengths is None else _ints(lengths, (c.seqs,), "lengths", index)
+        new = self.new_lengths[1 if at == self.new_at[0] else 0]
+        p.new_lengths = self.new_at[1 if at == self.new_at[0] else 0]
+        if self.rotary is not None:
+            shape = (rows,) if p.axes == 1 and positions is not None and positions.dim() == 1 else (p.axes, rows)
+            floats = positions is not None and positions.dtype is torch.float32
+            if positions is None or not _fits(positions, shape, torch.float32 if floats else torch.int32, index) or (
+                    rows > 1 and positions.stride()[-1] != 1):
+                raise ValueError("positions must be int32 or float32 [axes, rows] on the cache's device")
+            p.positions, p.positions_f32 = positions.data_ptr(), floats
+            p.axis_stride = positions.stride()[0]
+        _check(self.call(c.at, self.at, c.stream()), "sttm_cache_append")
         return AppendOutput(q_out, new, self.status)
 
 
@@ -190,7 +208,7 @@ class AttendPlan:
 
     def __init__(self, cache: PagedCache, q_heads: int, scale: Optional[float] = None, max_len: Optional[int] = None,
                  decay: float = 1.0):
-        self.cache, self.q_heads = cache, q_heads
+        self.cache, self.q_heads, self.shape = cache, q_heads, (cache.seqs, q_heads, cache.dim)
         self.max_len = cache.width * cache.page if max_len is None else int(max_len)
         self.out = torch.empty((cache.seqs, q_heads, cache.dim), dtype=cache.dtype, device=cache.device)
         self.lse = torch.empty((cache.seqs, q_heads), dtype=torch.float32, device=cache.device)
@@ -200,47 +218,47 @@ class AttendPlan:
         p.scale = 1.0 / math.sqrt(cache.dim) if scale is None else scale
         p.out, p.lse, p.device_status = self.out.data_ptr(), self.lse.data_ptr(), self.status.data_ptr()
         self.ws = {}
+        self.at, self.call = C.byref(p), binding.load_library().sttm_cache_attend
+        self.output = AttendOutput(self.out, self.lse, self.status)
 
-    def _workspace(self, scored: bool) -> torch.Tensor:
-        ws = self.ws.get(scored)
-        if ws is None:
-            n = int(binding.load_library().sttm_attend_workspace_bytes(C.byref(self.cache.struct), C.byref(self.params)))
-            # (0: the call itself names the reason)
-            ws = self.ws[scored] = torch.empty(max(n, 256), dtype=torch.uint8, device=self.cache.device)
-        return ws
+    def _workspace(self, scored: bool):
+        n = int(binding.load_library().sttm_attend_workspace_bytes(C.byref(self.cache.struct), C.byref(self.params)))
+        # (0: the call itself names the reason)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=self.cache.device)
+        self.ws[scored] = ws.data_ptr(), ws.numel(), ws
+        return self.ws[scored]
 
     def run(self, q: torch.Tensor, lengths: torch.Tensor, mask: Optional[torch.Tensor] = None,
             scores: Optional[torch.Tensor] = None) -> AttendOutput:
         """``q`` ``[seqs, q_heads, dim]``; ``lengths`` int32 ``[seqs]``; ``mask`` bool or uint8 ``[seqs, >= max_len]``,
         false: slot left out; ``scores`` float32 ``[seqs, heads, >= max_len]``, updated in place."""
         c, p = self.cache, self.params
-        c.on_current_device()
-        _want(q.shape == (c.seqs, self.q_heads, c.dim) and q.dtype == c.dtype and q.device == c.device and q.stride(2) == 1,
-              "q must be [seqs, q_heads, dim] of the cache's type, on its device, with contiguous channels")
-        s = q.stride()
-        p.q, p.q_seq, p.q_head = q.data_ptr(), s[0] if c.seqs > 1 else 0, s[1] if self.q_heads > 1 else 0
-        p.lengths = _ints(lengths, c.seqs, "lengths", c.device)
+        p.q, p.q_seq, p.q_head = _heads(q, self.shape, c.dtype, c.index, "q")
+        p.lengths = _ints(lengths, (c.seqs,), "lengths", c.index)
         if mask is None:
             p.mask = None
         else:
-            _want(mask.dim() == 2 and mask.shape[0] == c.seqs and mask.shape[1] >= self.max_len and mask.dtype in (torch.bool, torch.uint8)
-                  and mask.stride(1) == 1 and mask.device == c.device, "mask must be bool or uint8 [seqs, >= max_len] with contiguous rows")
-            p.mask, p.mask_stride = mask.data_ptr(), mask.stride(0)
+            stride = mask.stride()
+            if not (mask.dtype in (torch.bool, torch.uint8) and mask.dim() == 2 and mask.shape[0] == c.seqs
+                    and mask.shape[1] >= self.max_len and stride[1] == 1 and mask.get_device() == c.index):
+                raise ValueError("mask must be bool or uint8 [seqs, >= max_len] with contiguous rows, on the cache's device")
+            p.mask, p.mask_stride = mask.data_ptr(), stride[0]
         if scores is None:
             p.scores = None
         else:
-            _want_scores(scores, c, self.max_len)
-            p.scores, p.score_seq, p.score_head = scores.data_ptr(), scores.stride(0), scores.stride(1)
-        ws = self._workspace(scores is not None)
-        _check(binding.load_library().sttm_cache_attend(C.byref(c.struct), C.byref(p), ws.data_ptr(), ws.numel(), _stream()),
-               "sttm_cache_attend")
-        return AttendOutput(self.out, self.lse, self.status)
+            p.scores, p.score_seq, p.score_head = _scores(scores, c, self.max_len)
+        ws = self.ws.get(scores is not None) or self._workspace(scores is not None)
+        _check(self.call(c.at, self.at, ws[0], ws[1], c.stream()), "sttm_cache_attend")
+        return self.output
 
 
-def _want_scores(scores: torch.Tensor, c: PagedCache, max_len: int) -> None:
-    _want(scores.dim() == 3 and scores.shape[0] == c.seqs and scores.shape[1] == c.heads and scores.shape[2] >= max_len
-          and scores.dtype == torch.float32 and scores.stride(2) == 1 and scores.device == c.device,
-          "scores must be float32 [seqs, heads, >= max_len] with contiguous slots, on the cache's device")
+def _scores(t: torch.Tensor, c: PagedCache, max_len: int):
+    """Address, sequence stride and head stride of float32 [seqs, heads, >= max_len]."""
+    shape, stride = t.shape, t.stride()
+    if not (len(shape) == 3 and shape[0] == c.seqs and shape[1] == c.heads and shape[2] >= max_len and t.dtype is torch.float32
+            and stride[2] == 1 and t.get_device() == c.index):
+        raise ValueError("scores must be float32 [seqs, heads, >= max_len] with contiguous slots, on the cache's device")
+    return t.data_ptr(), stride[0], stride[1]
 
 
 @dataclass
@@ -265,6 +283,8 @@ class EvictPlan:
         self.new_scores = torch.empty(shape, dtype=torch.float32, device=src.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=src.device)
         p = self.params = EvictParams()
+        self.at, self.call = C.byref(p), binding.load_library().sttm_cache_evict
+        self.output = EvictOutput(self.new_lengths, self.kept, self.new_scores, self.status)
         p.max_len, p.first, p.last, p.kept_width = self.max_len, first, last, kept_width
         p.new_lengths, p.kept, p.new_scores = self.new_lengths.data_ptr(), self.kept.data_ptr(), self.new_scores.data_ptr()
         p.device_status = self.status.data_ptr()
@@ -272,14 +292,11 @@ class EvictPlan:
     def run(self, lengths: torch.Tensor, keep: torch.Tensor, scores: torch.Tensor) -> EvictOutput:
         """``lengths``, ``keep`` int32 ``[seqs]``; ``scores`` float32 ``[seqs, heads, >= max_len]``."""
         c, p = self.src, self.params
-        c.on_current_device()
-        p.lengths = _ints(lengths, c.seqs, "lengths", c.device)
-        p.keep = _ints(keep, c.seqs, "keep", c.device)
-        _want_scores(scores, c, self.max_len)
-        p.scores, p.score_seq, p.score_head = scores.data_ptr(), scores.stride(0), scores.stride(1)
-        _check(binding.load_library().sttm_cache_evict(C.byref(c.struct), C.byref(self.dst.struct), C.byref(p), _stream()),
-               "sttm_cache_evict")
-        return EvictOutput(self.new_lengths, self.kept, self.new_scores, self.status)
+        p.lengths = _ints(lengths, (c.seqs,), "lengths", c.index)
+        p.keep = _ints(keep, (c.seqs,), "keep", c.index)
+        p.scores, p.score_seq, p.score_head = _scores(scores, c, self.max_len)
+        _check(self.call(c.at, self.dst.at, self.at, c.stream()), "sttm_cache_evict")
+        return self.output
 
 
 def sttm_cache_append(cache: PagedCache, q, k, v, row_offsets, lengths=None, positions=None, rotary: Optional[Rotary] = None,
