@@ -308,17 +308,28 @@ sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const
     a.new_scores = p->new_scores;
     a.status = p->device_status;
     const long long rows = (long long)src->seqs * src->heads;
+    // CTAs per row: as few as hold its keys (more would only meet at more barriers), but more while the rows
+    // leave SMs idle
     int size = 1;
-    while (size < kSelMaxCluster && (long long)size * 8192 < p->max_len) size *= 2;
-    const long long per_thread = ((long long)p->max_len + (long long)size * kSelThreads - 1) / ((long long)size * kSelThreads) | 1;
-    a.slice_cap = (int)std::min<long long>(per_thread * kSelThreads, 48 * 1024);
-    static size_t allowed[kMaxDevices] = {};
-    const size_t smem = (size_t)a.slice_cap * 4;
-    if ((s = allow_smem((const void*)k_cache_select, smem, allowed)) != STTM_OK) return s;
-    if ((s = launch(k_cache_select, rows * size, kSelThreads, smem, (unsigned)size, stream, a)) != STTM_OK) return s;
+    while (size < kSelMaxCluster && ((long long)size * kSelThreads * kSelMaxKeys < p->max_len ||
+                                     (rows * size * 2 <= sm_count() && (long long)size * kSelThreads * 3 < p->max_len)))
+        size *= 2;
+    const long long per_thread = ((long long)p->max_len + (long long)size * kSelThreads - 1) / ((long long)size * kSelThreads);
+    auto select = [&](auto kpt) -> sttm_status {
+        constexpr int KPT = decltype(kpt)::value;
+        static size_t allowed[kMaxDevices] = {};
+        const size_t smem = KPT * kSelThreads * 4;
+        sttm_status r = allow_smem((const void*)k_cache_select<KPT>, smem, allowed);
+        return r != STTM_OK ? r : launch(k_cache_select<KPT>, rows * size, kSelThreads, smem, (unsigned)size, stream, a);
+    };
+    s = per_thread <= 3 ? select(std::integral_constant<int, 3>()) : per_thread <= 9 ? select(std::integral_constant<int, 9>())
+      : per_thread <= 17 ? select(std::integral_constant<int, 17>()) : per_thread <= 25 ? select(std::integral_constant<int, 25>())
+      : per_thread <= kSelMaxKeys ? select(std::integral_constant<int, kSelMaxKeys>())
+                                  : launch(k_cache_select_long, rows * size, kSelThreads, 0, (unsigned)size, stream, a);
+    if (s != STTM_OK) return s;
     return by_type(src, [&](auto, auto dim) {
         constexpr int D = decltype(dim)::value;
-        const int per_go = kMoveThreads / (D / 4) * 4;      // slots a block has in flight
+        const int per_go = kMoveWords * kMoveThreads / (D / 4);     // slots a block has in flight
         const long long go = (p->kept_width + per_go - 1) / per_go, fill = std::max<long long>(1, (long long)sm_count() * 32 / rows);
         const int chunks = (int)std::min(go, fill);
         return launch(k_cache_move<D>, rows * chunks, kMoveThreads, 0, 0, stream, a, chunks);
