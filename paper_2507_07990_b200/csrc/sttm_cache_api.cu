@@ -111,11 +111,11 @@ sttm_status make_cache_map(const sttm_cache* c, void* base, int box, CUtensorMap
     return r == CUDA_SUCCESS ? STTM_OK : STTM_ERR_UNSUPPORTED;      // (a stride beyond what a tensor map holds)
 }
 
-// Rows so short that one CTA takes each whole: nothing to join, one launch.
-constexpr int kWholeLen = 256;
+// Tiles per CTA up to which a row goes to one cluster while all clusters are resident at once.
+constexpr int kClusterTiles = 8;
 
 struct AttendPlan {
-    bool whole;
+    int cluster;                  // see AttendArgs
     long long tiles;              // upper bound over all rows
     int row_tiles, grid_limit;
     size_t rows, stats, partial, logits, total;
@@ -129,29 +129,41 @@ sttm_status plan_attend(const sttm_cache* c, const sttm_attend_params* p, Attend
     const int group = p->q_heads / c->heads;
     if (group > 64) return STTM_ERR_UNSUPPORTED;
     const long long rows = (long long)c->seqs * c->heads;
-    pl->row_tiles = (p->max_len + kAttTile - 1) / kAttTile;
+    const int tile = attend_tile(c->dim);
+    pl->row_tiles = (p->max_len + tile - 1) / tile;
     pl->tiles = rows * pl->row_tiles;
     if (pl->tiles > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
-    pl->whole = p->max_len <= kWholeLen;
     pl->grid_limit = sm_count() * (c->dim == 256 ? 1 : 2);
-    const long long parts = pl->whole ? rows : std::min<long long>(pl->grid_limit, pl->tiles) + rows;
+    // Clusters while that fills the GPU in one go with a few tiles per CTA (one launch, no partials in memory).
+    // 16 CTAs want 8 SMs of one GPC, or 16 where an SM holds one CTA: there 8 have to do.
+    const int most = c->dim == 256 ? 8 : kAttMaxCluster;
+    int size = 1;
+    while (size < most && size < pl->row_tiles && rows * size * 2 <= pl->grid_limit) size *= 2;
+    pl->cluster = pl->row_tiles <= size * kClusterTiles ? size : 0;
+    const long long parts = pl->cluster ? (pl->cluster == 1 ? rows : 0) : std::min<long long>(pl->grid_limit, pl->tiles) + rows;
     pl->rows = 0;
     pl->stats = align_up((size_t)rows * sizeof(int4));
     pl->partial = pl->stats + align_up((size_t)parts * group * sizeof(float2));
-    pl->logits = pl->partial + (pl->whole ? 0 : align_up((size_t)parts * group * c->dim * 4));
-    pl->total = pl->logits + (p->scores ? align_up((size_t)pl->tiles * group * kAttTile * 4) : 0);
+    pl->logits = pl->partial + (pl->cluster ? 0 : align_up((size_t)parts * group * c->dim * 4));
+    pl->total = pl->logits + (p->scores ? align_up((size_t)pl->tiles * group * tile * 4) : 0);
     return STTM_OK;
 }
 
 template <typename T, int DIM, int ROWS>
 sttm_status launch_attend(const AttendArgs& a, const AttendPlan& pl, const CUtensorMap& mk, const CUtensorMap& mv, void* stream) {
     static size_t allowed[kMaxDevices] = {};
-    const size_t smem = a.stages * attend_stage_bytes<DIM>() + attend_fixed_bytes<DIM, ROWS>();
+    const size_t smem = a.stages * kAttStage + attend_fixed_bytes<DIM, ROWS>();
     sttm_status s = allow_smem((const void*)k_cache_attend<T, DIM, ROWS>, smem, allowed);
     if (s != STTM_OK) return s;
+    if (pl.cluster > 8) {
+        static bool large[kMaxDevices] = {};
+        const int dev = device_slot();
+        if (!large[dev]) STTM_CUDA_TRY(cudaFuncSetAttribute(k_cache_attend<T, DIM, ROWS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        large[dev] = true;
+    }
     const long long rows = (long long)a.seqs * a.heads;
-    const long long grid = pl.whole ? rows : std::min<long long>(pl.grid_limit, pl.tiles);
-    return launch(k_cache_attend<T, DIM, ROWS>, grid, kAttThreads, smem, 0, stream, a, mk, mv);
+    const long long grid = pl.cluster ? rows * pl.cluster : std::min<long long>(pl.grid_limit, pl.tiles);
+    return launch(k_cache_attend<T, DIM, ROWS>, grid, kAttThreads, smem, (unsigned)pl.cluster, stream, a, mk, mv);
 }
 
 }  // namespace
@@ -241,9 +253,10 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
     a.seqs = cache->seqs;
     a.group = p->q_heads / cache->heads;
     // slots per copy: the largest power of two that divides a page, at most a tile
-    a.box = std::min(cache->page & -cache->page, kAttTile);
+    a.tile = attend_tile(cache->dim);
+    a.box = std::min(cache->page & -cache->page, a.tile);
     a.max_len = p->max_len;
-    a.whole = pl.whole;
+    a.cluster = pl.cluster;
     a.q = (const uint16_t*)p->q;
     a.q_seq = p->q_seq;
     a.q_head = p->q_head;
@@ -270,11 +283,13 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
         using T = decltype(tag);
         constexpr int D = decltype(dim)::value;
         // two CTAs to an SM with 96 KB of stages each, or one with 192 KB (256 channels)
-        a.stages = D == 64 ? 6 : 3;
+        a.stages = D == 256 ? 6 : 3;
         sttm_status r = a.group <= 8 ? launch_attend<T, D, 8>(a, pl, mk, mv, stream) : launch_attend<T, D, 16>(a, pl, mk, mv, stream);
-        if (r != STTM_OK || (pl.whole && p->scores == nullptr)) return r;
-        const long long join_blocks = pl.whole ? 0 : rows * a.group;
-        const int chunks = (p->max_len + kScoreChunk - 1) / kScoreChunk;
+        if (r != STTM_OK || pl.cluster) return r;
+        const long long join_blocks = rows * a.group;
+        // blocks per row that update scores: one slot per thread while that does not fill the GPU several times over
+        const int chunks = (int)std::min<long long>((p->max_len + kJoinThreads - 1) / kJoinThreads,
+                                                    std::max<long long>(1, (long long)sm_count() * 16 / rows));
         const long long grid = join_blocks + (p->scores ? rows * chunks : 0);
         return launch(k_cache_join<T, D>, grid, kJoinThreads, 0, 0, stream, a, (int)join_blocks, chunks);
     });
