@@ -217,7 +217,7 @@ sttm_status sttm_cache_append(const sttm_cache* cache, const sttm_append_params*
     a.eps = p->eps;
     a.status = p->device_status;
     // warps per row: one once the rows fill the GPU, else one per step of a row's heads
-    const int heads = p->q_heads + 2 * cache->heads, per_step = 32 / (cache->dim / 16), steps = (heads + per_step - 1) / per_step;
+    const int per_step = 32 / (cache->dim / 16), steps = (p->q_heads + per_step - 1) / per_step + 2 * ((cache->heads + per_step - 1) / per_step);
     const long long wanted = (long long)sm_count() * 32;
     a.parts = (int)std::min<long long>(steps, std::max<long long>(1, wanted / std::max<long long>(1, p->rows)));
     const long long grid = std::max<long long>(1, (p->rows * a.parts + kAppendWarps - 1) / kAppendWarps);
