@@ -19,6 +19,9 @@ import torch
 from . import binding
 from .binding import _check
 
+# Current device, and the current stream's handle alone: torch.cuda.current_stream() makes a stream object, which takes as
+# long as a small call does.
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 _DTYPES = {torch.bfloat16: 0, torch.float16: 2}
 
 
@@ -99,12 +102,8 @@ class PagedCache:
                                 _DTYPES[k.dtype])
         self.at = C.byref(self.struct)
 
-    def stream(self) -> int:
-        """The current stream of the cache's device, which has to be the current device."""
-        if torch._C._cuda_getDevice() != self.index:
-            raise ValueError("the cache is not on the current CUDA device")
-        # the handle alone: torch.cuda.current_stream() makes a stream object, which takes as long as a small call
-        return torch._C._cuda_getCurrentRawStream(self.index)
+    def other_device(self) -> None:
+        raise ValueError("the cache is not on the current CUDA device")
 
 
 def empty_cache(seqs: int, max_len: int, heads: int, dim: int, page: int = 64, dtype: torch.dtype = torch.bfloat16,
@@ -143,6 +142,7 @@ class AppendPlan:
         self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
         p = self.params = AppendParams()
         self.at, self.call = C.byref(p), binding.load_library().sttm_cache_append
+        self.output = AppendOutput(None, None, self.status)
         p.q_heads, p.eps, p.axes = q_heads, eps, 1
         p.device_status = self.status.data_ptr()
         if rotary is not None:
@@ -165,8 +165,8 @@ class AppendPlan:
             q_out: Optional[torch.Tensor] = None) -> AppendOutput:
         """``q`` ``[rows, q_heads, dim]``, ``k``, ``v`` ``[rows, heads, dim]`` (any row and head strides, views of one
         projection for instance); ``row_offsets`` int64 ``[seqs + 1]``; ``lengths`` int32 ``[seqs]`` (None: an empty cache);
-        ``positions`` int32 or float32 ``[rows]`` or ``[axes, rows]``.  ``new_lengths`` of the result is valid until
-        the call after the next."""
+        ``positions`` int32 or float32 ``[rows]`` or ``[axes, rows]``.  The plan returns the same object every time;
+        the ``new_lengths`` tensor it names is written again by the call after the next."""
         c, p = self.cache, self.params
         dim, dtype, index, rows = c.dim, c.dtype, c.index, k.shape[0]
         if self.q_heads > 0:
@@ -182,8 +182,9 @@ class AppendPlan:
             raise ValueError("row_offsets must be a contiguous int64 tensor [seqs + 1] on the cache's device")
         p.row_offsets, p.rows = row_offsets.data_ptr(), rows
         p.lengths = at = None if lengths is None else _ints(lengths, (c.seqs,), "lengths", index)
-        new = self.new_lengths[1 if at == self.new_at[0] else 0]
-        p.new_lengths = self.new_at[1 if at == self.new_at[0] else 0]
+        which = 1 if at == self.new_at[0] else 0
+        new = self.new_lengths[which]
+        p.new_lengths = self.new_at[which]
         if self.rotary is not None:
             shape = (rows,) if p.axes == 1 and positions is not None and positions.dim() == 1 else (p.axes, rows)
             floats = positions is not None and positions.dtype is torch.float32
@@ -192,8 +193,14 @@ class AppendPlan:
                 raise ValueError("positions must be int32 or float32 [axes, rows] on the cache's device")
             p.positions, p.positions_f32 = positions.data_ptr(), floats
             p.axis_stride = positions.stride()[0]
-        _check(self.call(c.at, self.at, c.stream()), "sttm_cache_append")
-        return AppendOutput(q_out, new, self.status)
+        if _device() != index:
+            c.other_device()
+        code = self.call(c.at, self.at, _raw_stream(index))
+        if code:
+            _check(code, "sttm_cache_append")
+        out = self.output
+        out.q, out.new_lengths = q_out, new
+        return out
 
 
 @dataclass
@@ -248,7 +255,11 @@ class AttendPlan:
         else:
             p.scores, p.score_seq, p.score_head = _scores(scores, c, self.max_len)
         ws = self.ws.get(scores is not None) or self._workspace(scores is not None)
-        _check(self.call(c.at, self.at, ws[0], ws[1], c.stream()), "sttm_cache_attend")
+        if _device() != c.index:
+            c.other_device()
+        code = self.call(c.at, self.at, ws[0], ws[1], _raw_stream(c.index))
+        if code:
+            _check(code, "sttm_cache_attend")
         return self.output
 
 
@@ -295,7 +306,11 @@ class EvictPlan:
         p.lengths = _ints(lengths, (c.seqs,), "lengths", c.index)
         p.keep = _ints(keep, (c.seqs,), "keep", c.index)
         p.scores, p.score_seq, p.score_head = _scores(scores, c, self.max_len)
-        _check(self.call(c.at, self.dst.at, self.at, c.stream()), "sttm_cache_evict")
+        if _device() != c.index:
+            c.other_device()
+        code = self.call(c.at, self.dst.at, self.at, _raw_stream(c.index))
+        if code:
+            _check(code, "sttm_cache_evict")
         return self.output
 
 

@@ -287,9 +287,9 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
         sttm_status r = a.group <= 8 ? launch_attend<T, D, 8>(a, pl, mk, mv, stream) : launch_attend<T, D, 16>(a, pl, mk, mv, stream);
         if (r != STTM_OK || pl.cluster) return r;
         const long long join_blocks = rows * a.group;
-        // blocks per row that update scores: one slot per thread while that does not fill the GPU several times over
-        const int chunks = (int)std::min<long long>((p->max_len + kJoinThreads - 1) / kJoinThreads,
-                                                    std::max<long long>(1, (long long)sm_count() * 16 / rows));
+        // blocks per row that update scores: one go each while all of them are resident at once
+        const int chunks = (int)std::min<long long>((p->max_len + kScoreSlots - 1) / kScoreSlots,
+                                                    std::max<long long>(1, (long long)sm_count() * 8 / rows));
         const long long grid = join_blocks + (p->scores ? rows * chunks : 0);
         return launch(k_cache_join<T, D>, grid, kJoinThreads, 0, 0, stream, a, (int)join_blocks, chunks);
     });

@@ -49,6 +49,7 @@ constexpr int kJoinRegs = 16;                               // output registers 
 constexpr int kAttMaxCluster = 16;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kJoinThreads = 256;
+constexpr int kScoreSlots = 2 * kJoinThreads;               // slots whose scores a block updates in one go
 
 struct AttendArgs {
     const int32_t* table;
@@ -807,7 +808,7 @@ __device__ __forceinline__ float2 join_stats(const AttendArgs& p, const int4& r,
 // The end of a call: rows that were split are joined (a block per row and query head), and with scores
 // every slot's weight is added to its score (`chunks` blocks per row).
 template <typename T, int DIM>
-__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const __grid_constant__ AttendArgs p, int join_blocks, int chunks) {
+__global__ void __launch_bounds__(kJoinThreads, 4) k_cache_join(const __grid_constant__ AttendArgs p, int join_blocks, int chunks) {
     constexpr int LANES = DIM / 4;                          // threads that hold one head's channels, four each
     constexpr int PARTS = kJoinThreads / LANES;
     __shared__ float4 acc[kJoinThreads];
@@ -852,20 +853,25 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const __grid_consta
         }
         return;
     }
-    // a thread per slot; its logits (the first eight heads') are on their way while the statistics are joined
+    // two slots to a thread at a time; their logits (the first eight heads') are on their way while the statistics
+    // are joined
     const int k = blockIdx.x - join_blocks, row = k / chunks;
-    int slot = (k % chunks) * kJoinThreads + threadIdx.x;
+    int slot0 = (k % chunks) * kScoreSlots;
     const int b = row / p.heads;
     const int4 r = p.rows[row];
     const int len = attend_length(p, b);
-    if (slot - (int)threadIdx.x >= len) return;
+    if (slot0 >= len) return;
     float* score = p.scores + b * p.score_seq + (row % p.heads) * p.score_head;
-    float v[8], before = 0.f;
+    float v[2][8], before[2] = {0.f, 0.f};
     auto ask = [&](int g0) {
-        const float* x = p.logits + ((long long)(r.x + slot / p.tile) * p.group + g0) * p.tile + slot % p.tile;
 #pragma unroll
-        for (int g = 0; g < 8; g++) v[g] = slot < len && g0 + g < p.group ? __ldcg(x + g * p.tile) : -INFINITY;
-        if (g0 == 0 && slot < len) before = score[slot];
+        for (int u = 0; u < 2; u++) {
+            const int slot = slot0 + u * kJoinThreads + threadIdx.x;
+            const float* x = p.logits + ((long long)(r.x + slot / p.tile) * p.group + g0) * p.tile + slot % p.tile;
+#pragma unroll
+            for (int g = 0; g < 8; g++) v[u][g] = slot < len && g0 + g < p.group ? __ldcg(x + g * p.tile) : -INFINITY;
+            if (g0 == 0 && slot < len) before[u] = score[slot];
+        }
     };
     ask(0);
     for (int h = warp; h < p.group; h += kJoinThreads / 32) {
@@ -873,18 +879,23 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const __grid_consta
         if (lane == 0) stat[h] = weight_of(st.x, st.y);
     }
     __syncthreads();
-    for (; slot < len; slot += chunks * kJoinThreads) {
-        if (slot >= chunks * kJoinThreads) ask(0);
-        float w = 0.f;
+    for (bool first = true; slot0 < len; slot0 += chunks * kScoreSlots, first = false) {
+        if (!first) ask(0);
+        float w[2] = {0.f, 0.f};
         for (int g0 = 0; g0 < p.group; g0 += 8) {
 #pragma unroll
             for (int g = 0; g < 8; g++) {
                 const float2 st = stat[min(g0 + g, p.group - 1)];
-                w = fmaf(exp2_weight(v[g] - st.x), st.y, w);
+#pragma unroll
+                for (int u = 0; u < 2; u++) w[u] = fmaf(exp2_weight(v[u][g] - st.x), st.y, w[u]);
             }
             if (g0 + 8 < p.group) ask(g0 + 8);
         }
-        score[slot] = fmaf(p.decay, before, w);
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const int slot = slot0 + u * kJoinThreads + threadIdx.x;
+            if (slot < len) score[slot] = fmaf(p.decay, before[u], w[u]);
+        }
     }
 }
 
