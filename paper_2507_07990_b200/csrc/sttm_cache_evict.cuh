@@ -202,12 +202,13 @@ __device__ __forceinline__ uint2 select_before(SelectShared& sh, const SelectRow
     if (r.size == 1) return before;
     if (threadIdx.x == 0) sh.counts = total;
     cluster_barrier();
-    for (int k = 0; k < r.rank; k++) {
+    // a lane per CTA before this one
+    const int k = threadIdx.x & 31;
+    if (k < r.rank) {
         const uint32_t at = map_to_rank(smem_u32(&sh.counts), k);
-        before.x += dsmem_load(at);
-        before.y += dsmem_load(at + 4);
+        before = make_uint2(dsmem_load(at), dsmem_load(at + 4));
     }
-    return before;
+    return make_uint2(__reduce_add_sync(0xffffffffu, before.x), __reduce_add_sync(0xffffffffu, before.y));
 }
 
 // the radix steps: bits that the steps before have fixed, lowest bit of the step's digit, its mask
@@ -273,10 +274,19 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(const __grid_const
             e += equal;
         }
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < chosen; i += kSelThreads) {
-            const int slot = (int)keys[i];
-            r.kept[base + i] = r.lo + slot;
-            r.out[base + i] = __ldcg(r.score + slot);
+        for (uint32_t i0 = threadIdx.x; i0 < chosen; i0 += 4 * kSelThreads) {       // (four scores on their way at once)
+            float x[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if (i0 + u * kSelThreads < chosen) x[u] = __ldcg(r.score + (int)keys[i0 + u * kSelThreads]);
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const uint32_t i = i0 + u * kSelThreads;
+                if (i < chosen) {
+                    r.kept[base + i] = r.lo + (int)keys[i];
+                    r.out[base + i] = x[u];
+                }
+            }
         }
     }
     if (r.size > 1) cluster_barrier();                      // nobody leaves while its counts may be read
