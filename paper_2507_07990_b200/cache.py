@@ -137,9 +137,10 @@ class AppendPlan:
                  k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
         self.cache, self.q_heads, self.rotary, self.keep = cache, q_heads, rotary, (q_norm, k_norm)
         # two of them: the lengths that a call reads may be those that the call before it wrote
-        self.new_lengths = [torch.zeros(cache.seqs, dtype=torch.int32, device=cache.device) for _ in range(2)]
+        n = cache.seqs
+        ints = torch.zeros(2 * n + 1, dtype=torch.int32, device=cache.device)
+        self.new_lengths, self.status = [ints[:n], ints[n:2 * n]], ints[2 * n:]
         self.new_at = [t.data_ptr() for t in self.new_lengths]
-        self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
         p = self.params = AppendParams()
         self.at, self.call = C.byref(p), binding.load_library().sttm_cache_append
         self.output = AppendOutput(None, None, self.status)
