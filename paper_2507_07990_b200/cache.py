@@ -315,6 +315,10 @@ class EvictPlan:
         return self.output
 
 
+def _room(cache: PagedCache, max_len: Optional[int], *per_slot) -> int:
+    return min([cache.width * cache.page] + [t.shape[-1] for t in per_slot if t is not None]) if max_len is None else max_len
+
+
 def sttm_cache_append(cache: PagedCache, q, k, v, row_offsets, lengths=None, positions=None, rotary: Optional[Rotary] = None,
                       q_norm=None, k_norm=None, eps: float = 1e-6) -> AppendOutput:
     """Norm, rotation and cache entry of new tokens; see AppendPlan.run."""
@@ -323,11 +327,14 @@ def sttm_cache_append(cache: PagedCache, q, k, v, row_offsets, lengths=None, pos
 
 def sttm_cache_attend(cache: PagedCache, q, lengths, mask=None, scores=None, scale: Optional[float] = None,
                       max_len: Optional[int] = None, decay: float = 1.0) -> AttendOutput:
-    """Attention of one new token per sequence; see AttendPlan.run."""
+    """Attention of one new token per sequence; see AttendPlan.run.  ``max_len`` None: what the table, and the mask and
+    the scores, have room for."""
+    max_len = _room(cache, max_len, mask, scores)
     return AttendPlan(cache, q.shape[1], scale, max_len, decay).run(q, lengths, mask, scores)
 
 
 def sttm_cache_evict(src: PagedCache, dst: PagedCache, lengths, keep, scores, kept_width: int, first: int = 0, last: int = 0,
                      max_len: Optional[int] = None) -> EvictOutput:
-    """Keeps the highest-scored slots; see EvictPlan.run."""
+    """Keeps the highest-scored slots; see EvictPlan.run.  ``max_len`` None: what the table and the scores have room for."""
+    max_len = _room(src, max_len, scores)
     return EvictPlan(src, dst, kept_width, first, last, max_len).run(lengths, keep, scores)
