@@ -111,8 +111,12 @@ sttm_status make_cache_map(const sttm_cache* c, void* base, int box, CUtensorMap
     return r == CUDA_SUCCESS ? STTM_OK : STTM_ERR_UNSUPPORTED;      // (a stride beyond what a tensor map holds)
 }
 
-// Tiles per CTA up to which a row goes to one cluster while all clusters are resident at once.
-constexpr int kClusterTiles = 8;
+// Rows go to clusters (one launch, no parts in memory) up to so many tiles per CTA; beyond, equal shares spread them over
+// more SMs.  4 rows in clusters of 16: 4096 slots 10.5 us against 10.5 to 11.5 (the second launch's cost on the host varies), 8192
+// slots 12.9 against 11.9.  Where the rows alone occupy half of the GPU's CTAs, a CTA takes a row up to kWholeTiles tiles: 256 rows
+// of 512 slots 18 us against 30, of 1024 30 against 41; of 2048 53 both ways.  With scores only the latter: a cluster's
+// few threads take longer over the scores than the launch that spares them (4 rows of 4096 slots: 13.2 us against 12.1).
+constexpr int kClusterTiles = 6, kWholeTiles = 16;
 
 struct AttendPlan {
     int cluster;                  // see AttendArgs
@@ -134,12 +138,13 @@ sttm_status plan_attend(const sttm_cache* c, const sttm_attend_params* p, Attend
     pl->tiles = rows * pl->row_tiles;
     if (pl->tiles > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
     pl->grid_limit = sm_count() * (c->dim == 256 ? 1 : 2);
-    // Clusters while that fills the GPU in one go with a few tiles per CTA (one launch, no partials in memory).
-    // 16 CTAs want 8 SMs of one GPC, or 16 where an SM holds one CTA: there 8 have to do.
+    // The largest cluster that leaves every CTA a tile and, over all rows, an SM.  16 CTAs want 8 SMs of one GPC, or 16
+    // where an SM holds one CTA: there 8 have to do.
     const int most = c->dim == 256 ? 8 : kAttMaxCluster;
     int size = 1;
-    while (size < most && size < pl->row_tiles && rows * size * 2 <= pl->grid_limit) size *= 2;
-    pl->cluster = pl->row_tiles <= size * kClusterTiles ? size : 0;
+    while (size < most && size < pl->row_tiles && rows * size * 2 <= sm_count()) size *= 2;
+    const bool many = rows * 2 > pl->grid_limit;
+    pl->cluster = pl->row_tiles <= size * (many ? kWholeTiles : kClusterTiles) && (many || p->scores == nullptr) ? size : 0;
     const long long parts = pl->cluster ? (pl->cluster == 1 ? rows : 0) : std::min<long long>(pl->grid_limit, pl->tiles) + rows;
     pl->rows = 0;
     pl->stats = align_up((size_t)rows * sizeof(int4));

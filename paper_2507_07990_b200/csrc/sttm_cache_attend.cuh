@@ -6,26 +6,26 @@
 // and everything else is small, so HBM bounds the kernel as long as the products keep up: the group of
 // query heads that share a KV head forms the rows of one small matrix product per 16 slots.
 //
-// *Split.*  Two ways.  Equal shares: the slots of all (sequence, KV head) rows are cut into tiles and laid end to end; CTA
-// i takes the i-th of equal shares, whatever rows they belong to.  So one long sequence or many ragged
-// ones keep every SM streaming equally long; a row that lies in several shares leaves a running
-// maximum, a sum and an unscaled output per share, joined in share order by k_cache_join (no
-// atomics: the bits of a result do not depend on scheduling).  Clusters: a row is cut evenly over the 1 to 16 CTAs of a
-// cluster, which join their parts in shared memory, one launch in all.  The host's rule is in plan_attend().
+// *Split.*  Two ways, by the rule in plan_attend().  Equal shares: the slots of all (sequence, KV head) rows are cut
+// into tiles and laid end to end; CTA i takes the i-th of equal shares, whatever rows they belong to.  So one long
+// sequence or many ragged ones keep every SM streaming equally long; a row that lies in several shares leaves a running
+// maximum, a sum and an unscaled output per share, joined in share order by k_cache_join (no atomics: the bits of a
+// result do not depend on scheduling).  Clusters: a row is cut evenly over the 1 to 16 CTAs of a cluster, which join
+// their parts in shared memory, one launch in all.  5338 slots of 4 KV heads: 11.9 us in clusters of 16, 14 us in shares.
 //
-// *Pipeline.*  A producer warp brings a tile's keys and values (32 KB) into a ring of shared-memory stages by
-// tensor copies, one box of slots that lie in one page per copy, under the 128-byte swizzle; boxes whose slots are
-// all masked are not copied.  Four warps take 32 slots at a time and never wait for one another before the end
-// of a row: each keeps its own maximum, sum and output.  (With 16 slots to a warp, a tile took 1400 cycles from its
-// arrival to its release, whatever it weighed: one chain of eight dependent products, a maximum, a chain of exponentials.)
+// *Pipeline.*  A producer warp brings a tile's keys and values (32 KB) into a ring of shared-memory stages by tensor
+// copies, one box of slots that lie in one page per copy, under the 128-byte swizzle; boxes whose slots are all masked
+// are not copied.  Four warps take 32 slots at a time and never wait for one another before the end of a row: each keeps
+// its own maximum, sum and output.  32 x 32700 slots of 8 KV heads (4.3 GB) stream at 6.9 TB/s, as fast as this memory
+// reads; with scores (their logits are written and read once more, 0.5 GB) the call takes 732 us instead of 620.
 //
-// *Products.*  S = Q K^T and O += P V on mma.sync m16n8k16 with fp32 sums.  P is not rounded to 16
-// bits: it enters as hi + lo, two 16-bit numbers that hold 16 bits of it (22 in fp16).  With
-// at most 8 heads (ROWS = 8) the remainder travels in the idle rows 8 ... 15 of the same product and costs
-// nothing.  In fp16 the running maximum stands for 2^15, so that weights down to 2^-29 of the largest stay clear
-// of the subnormals.
-// The fifth-generation product (tcgen05.mma) needs 64 rows: with 7 heads nine tenths of it would be
-// padding, and at 8 KB of cache per 32 products the legacy pipe is busy a fifth of the streaming time.
+// *Products.*  S = Q K^T and O += P V on mma.sync m16n8k16 with fp32 sums.  P is not rounded to 16 bits: it enters as
+// hi + lo, two 16-bit numbers that hold 16 bits of it (22 in fp16).  With at most 8 heads (ROWS = 8) the remainder travels
+// in the idle rows 8 ... 15 of the same product and costs nothing.  In fp16 the running maximum stands for 2^15, so that
+// weights down to 2^-29 of the largest stay clear of the subnormals.  A warp needs some 1800 cycles for its 32 slots of
+// 128 channels, a quarter of the time that HBM needs for an SM's share of them: the fifth-generation products, whose
+// accumulators would have to travel through tensor memory twice per tile, have nothing to win here (the tensor pipe is busy
+// 19 % of the streaming time).
 #pragma once
 
 #include <cuda.h>
@@ -140,58 +140,88 @@ struct Cursor {
     }
 };
 
-// A CTA's tiles [t0, t1), where they begin, and how many a CTA takes (equal shares).  Every warp works it out.
+// A CTA's tiles [t0, t1) and where they begin.  Every warp works it out.
 struct Share {
-    int t0, t1, each;
+    int t0, t1, each;             // each: tiles of a share
+    int first_cta, parts;         // of the row, when shares end with rows; else parts = 0
     Cursor c;
 };
+__device__ __forceinline__ int tiles_of(const AttendArgs& p, int len) { return (len + p.tile - 1) / p.tile; }
 __device__ __forceinline__ Share attend_share(const AttendArgs& p, int cta, int lane) {
     Share s;
     if (p.cluster > 0) {
-        const int row = cta / p.cluster, rank = cta - row * p.cluster, base = row * ((p.max_len + p.tile - 1) / p.tile);
+        const int row = cta / p.cluster, rank = cta - row * p.cluster, base = row * tiles_of(p, p.max_len);
         s.c.b = row / p.heads;
         s.c.h = row - s.c.b * p.heads;
         s.c.len = attend_length(p, s.c.b);
-        s.c.tiles = (s.c.len + p.tile - 1) / p.tile;
+        s.c.tiles = tiles_of(p, s.c.len);
         s.c.j = (int)((long long)s.c.tiles * rank / p.cluster);
         s.t0 = base + s.c.j;
         s.t1 = base + (int)((long long)s.c.tiles * (rank + 1) / p.cluster);
         s.each = 1;
+        s.first_cta = cta;
+        s.parts = 1;
         return s;
     }
-    // tiles of 32 sequences at a time; with at most 32 the second pass finds them in registers
-    int len = lane < p.seqs ? attend_length(p, lane) : 0, tiles = (len + p.tile - 1) / p.tile;
-    int total = __reduce_add_sync(0xffffffffu, tiles * p.heads);
-    for (int b0 = 32; b0 < p.seqs; b0 += 32)
-        total += __reduce_add_sync(0xffffffffu, b0 + lane < p.seqs ? (attend_length(p, b0 + lane) + p.tile - 1) / p.tile * p.heads : 0);
-    s.each = max(1, (total + (int)gridDim.x - 1) / (int)gridDim.x);
-    s.t0 = (int)min((long long)cta * s.each, (long long)total);
-    s.t1 = min(s.t0 + s.each, total);
-    s.c.b = s.c.h = s.c.j = s.c.len = s.c.tiles = 0;
-    int base = 0;
-    for (int b0 = 0; s.t0 < s.t1; b0 += 32) {
-        if (b0 > 0) {
-            len = b0 + lane < p.seqs ? attend_length(p, b0 + lane) : 0;
-            tiles = (len + p.tile - 1) / p.tile;
+    // 32 sequences at a time; with at most 32 everything stays in registers
+    const int len0 = lane < p.seqs ? attend_length(p, lane) : 0, tiles0 = tiles_of(p, len0);
+    auto sum = [&](auto&& f) {
+        int total = __reduce_add_sync(0xffffffffu, f(tiles0));
+        for (int b0 = 32; b0 < p.seqs; b0 += 32)
+            total += __reduce_add_sync(0xffffffffu, f(b0 + lane < p.seqs ? tiles_of(p, attend_length(p, b0 + lane)) : 0));
+        return total * p.heads;
+    };
+    const int grid = (int)gridDim.x, total = sum([](int tiles) { return tiles; });
+    s.each = max(1, (total + grid - 1) / grid);
+    // Shares that end with their rows, if somewhat longer ones make room for that: a share of parts of two rows pays
+    // for a second end and start, during which its copies stall (256 rows of 4096 slots: 89 us instead of 101).  Short
+    // shares would grow by too much, and under a mask tiles are not equal (48 ragged masked rows: 30 us instead of 28).
+    bool with_rows = false;
+    for (int k = 0; k < 4 && s.each >= 6 && p.mask == nullptr && !with_rows; k++) {
+        const int e = s.each + k * (s.each / 6) / 3;        // up to a sixth more
+        if (sum([e](int tiles) { return (tiles + e - 1) / e; }) <= (int)gridDim.x) {
+            with_rows = true;
+            s.each = e;
         }
-        const int n = tiles * p.heads;
-        int upto = n;                                       // inclusive prefix sum
+    }
+    // the sequence that this CTA's share begins in: a prefix sum of shares (of tiles, where shares run on)
+    const int at = with_rows ? cta : (int)min((long long)cta * s.each, (long long)total);
+    s.t0 = s.t1 = s.first_cta = s.parts = 0;
+    s.c.b = s.c.h = s.c.j = s.c.len = s.c.tiles = 0;
+    int base = 0, base_tiles = 0;
+    for (int b0 = 0; b0 < p.seqs; b0 += 32) {
+        const int len = b0 == 0 ? len0 : (b0 + lane < p.seqs ? attend_length(p, b0 + lane) : 0), tiles = b0 == 0 ? tiles0 : tiles_of(p, len);
+        const int per_row = with_rows ? (tiles + s.each - 1) / s.each : tiles;
+        int upto = per_row * p.heads, upto_tiles = tiles * p.heads;         // inclusive prefix sums
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
+            const int v = __shfl_up_sync(0xffffffffu, upto, o), w = __shfl_up_sync(0xffffffffu, upto_tiles, o);
+            if (lane >= o) {
+                upto += v;
+                upto_tiles += w;
+            }
         }
-        const unsigned past = __ballot_sync(0xffffffffu, base + upto > s.t0);
+        const unsigned past = __ballot_sync(0xffffffffu, base + upto > at);
         if (past != 0) {
-            const int at = __ffs(past) - 1, off = s.t0 - base - __shfl_sync(0xffffffffu, upto - n, at);
-            s.c.b = b0 + at;
-            s.c.len = __shfl_sync(0xffffffffu, len, at);
-            s.c.tiles = __shfl_sync(0xffffffffu, tiles, at);
-            s.c.h = off / s.c.tiles;
-            s.c.j = off - s.c.h * s.c.tiles;
+            const int owner = __ffs(past) - 1, n = __shfl_sync(0xffffffffu, per_row, owner);
+            const int off = at - base - __shfl_sync(0xffffffffu, upto - per_row * p.heads, owner);
+            s.c.b = b0 + owner;
+            s.c.len = __shfl_sync(0xffffffffu, len, owner);
+            s.c.tiles = __shfl_sync(0xffffffffu, tiles, owner);
+            s.c.h = off / n;
+            const int k = off - s.c.h * n;                  // share (tile) of the row
+            const int row_tile = base_tiles + __shfl_sync(0xffffffffu, upto_tiles - tiles * p.heads, owner) + s.c.h * s.c.tiles;
+            s.c.j = with_rows ? k * s.each : k;
+            s.t0 = row_tile + s.c.j;
+            s.t1 = min(s.t0 + s.each, with_rows ? row_tile + s.c.tiles : total);
+            if (with_rows) {
+                s.first_cta = cta - k;
+                s.parts = n;
+            }
             break;
         }
         base += __shfl_sync(0xffffffffu, upto, 31);
+        base_tiles += __shfl_sync(0xffffffffu, upto_tiles, 31);
     }
     return s;
 }
@@ -245,7 +275,7 @@ __device__ __forceinline__ void attend_leave_nothing(const AttendArgs& p, uint32
 }
 // by all threads of all CTAs of the cluster
 template <typename T, int DIM>
-__device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine, int first_tile, int logits_tile, int tiles) {
+__device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine, int logits_tile, int tiles) {
     const uint32_t at = smem_u32(mine);
     const int rank = blockIdx.x % p.cluster, row = blockIdx.x / p.cluster, lane = threadIdx.x & 31;
     // behind this CTA's part: what every part's outputs count in the end [cluster][group], and the final statistics
@@ -296,6 +326,7 @@ __device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine
         if (i + kAttThreads < end) ask(i + kAttThreads);
     }
     if (p.logits != nullptr && tiles > 0) {
+        const int first_tile = logits_tile - row * tiles_of(p, p.max_len);      // of this CTA in the row
         const int b = row / p.heads, from = first_tile * p.tile;
         add_scores(p, b, row % p.heads, from, min(attend_length(p, b), from + tiles * p.tile), logits_tile - first_tile, final_stat, threadIdx.x,
                    kAttThreads);
@@ -339,9 +370,21 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
     __syncthreads();
     wait_for_prior_kernel();
     let_next_kernel_start();
-    Share sh = attend_share(p, cta, lane);
-    const int t0 = sh.t0, t1 = sh.t1, j0 = sh.c.j;
-    Cursor& c = sh.c;
+    __shared__ int share_info[4];                           // what only a row's end needs, out of the loops' registers
+    Cursor c;
+    int t0, t1;
+    {
+        const Share sh = attend_share(p, cta, lane);
+        c = sh.c;
+        t0 = sh.t0;
+        t1 = sh.t1;
+        if (threadIdx.x == 0) {
+            share_info[0] = sh.each;
+            share_info[1] = sh.first_cta;
+            share_info[2] = sh.parts;
+        }
+        if (warp < kAttWarps) named_sync(1, kAttWarps * 32);
+    }
     bool timed_out = false;
 
     if (warp == kAttWarps) {
@@ -457,7 +500,7 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
             }
         }
         if (timed_out && lane == 0) raise_status(p.status, kStatusWaitTimeout);
-        if (p.cluster > 1) attend_join_cluster<T, DIM>(p, ring_ptr, j0, t0, t1 - t0);
+        if (p.cluster > 1) attend_join_cluster<T, DIM>(p, ring_ptr, t0, t1 - t0);
         return;
     }
 
@@ -676,8 +719,8 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
             }
             const int row = c.b * p.heads + c.h;
             const int first = part - c.j;                   // the row's first tile
-            const int first_cta = p.cluster ? cta : first / sh.each;
-            const int parts = p.cluster ? 1 : (first + c.tiles - 1) / sh.each - first_cta + 1;
+            const int each = share_info[0], first_cta = share_info[2] ? share_info[1] : first / each;
+            const int parts = share_info[2] ? share_info[2] : (first + c.tiles - 1) / each - first_cta + 1;
             const long long at = (long long)(cta + (p.cluster ? 0 : row));      // grows along the staircase of (CTA, row) pairs: unique
             constexpr int COLS = 8 * kJoinRegs / OR, STRIDE = COLS + 8;         // channels per round; padded: no bank conflict
             // every warp brings its outputs to the row's common reference first
@@ -777,7 +820,7 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
             if (p.lengths[b] < 0 || p.lengths[b] > p.max_len) raise_status(p.status, kStatusCapacity);
     if (p.cluster > 1) {
         if (t0 >= t1) attend_leave_nothing<DIM>(p, ring);
-        attend_join_cluster<T, DIM>(p, ring_ptr, j0, t0, t1 - t0);
+        attend_join_cluster<T, DIM>(p, ring_ptr, t0, t1 - t0);
     }
 }
 

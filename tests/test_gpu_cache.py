@@ -244,6 +244,28 @@ def test_attend_one_long_sequence(case):
     check_attend(p, run_attend(p), before)
 
 
+@pytest.mark.parametrize("case", [dict(q_heads=7, dim=128), dict(q_heads=20, heads=1, dtype="f16"), dict(q_heads=40, dim=128, order="slots", page=48)], ids=str)
+def test_attend_rows_joined_in_large_clusters(case):
+    # clusters of 16 CTAs, under a mask of whole stretches (copies left out) whose rows begin at odd addresses
+    p = attend_problem(34, (4003, 2999, 100), masked=0.0, **case)
+    p["mask"] &= (torch.rand((3, 4003 // 37 + 1), generator=torch.Generator().manual_seed(1)) < 0.5).cuda().repeat_interleave(37, 1)[:, :4003]
+    check_attend(p, run_attend(p))
+    p["scores"] = torch.rand((3, 1, 4003), device="cuda")
+    before = p["scores"].clone()
+    check_attend(p, run_attend(p), before)
+
+
+@pytest.mark.parametrize("scored", [False, True])
+def test_attend_a_cta_per_row(scored):
+    # rows enough to fill the GPU: whole rows to single CTAs; and longer ones in shares that end with rows
+    rng = np.random.RandomState(5)
+    for most, heads in ((700, 8), (1500, 8)):
+        lens = [most] + [int(x) for x in rng.randint(most // 2, most, 21)]
+        p = attend_problem(35, lens, q_heads=16, heads=heads, dim=64, page=32, scored=scored)
+        before = None if p["scores"] is None else p["scores"].clone()
+        check_attend(p, run_attend(p), before)
+
+
 def test_attend_more_sequences_than_a_warp_scans_at_once():
     rng = np.random.RandomState(3)
     lens = [int(x) for x in rng.randint(0, 400, 90)]
