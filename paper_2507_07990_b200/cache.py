@@ -61,19 +61,15 @@ def _want(ok: bool, text: str) -> None:
         raise ValueError(text)
 
 
-def _fits(t: torch.Tensor, shape: tuple, dtype: torch.dtype, index: int) -> bool:
-    return t.dtype is dtype and t.shape == shape and t.get_device() == index
-
-
 def _ints(t: torch.Tensor, shape: tuple, what: str, index: int) -> int:
-    if not (_fits(t, shape, torch.int32, index) and t.is_contiguous()):
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 tensor [%d] on the cache's device" % (what, shape[0]))
     return t.data_ptr()
 
 
 def _heads(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, index: int, what: str):
     """Address, row stride and head stride of [rows, heads, dim] (any strides of the first two axes)."""
-    if t is None or not _fits(t, shape, dtype, index):
+    if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         raise ValueError("%s must be a %s tensor %s on the cache's device" % (what, dtype, list(shape)))
     row, head, channel = t.stride()
     if channel != 1 and shape[0] > 0:
@@ -143,7 +139,7 @@ class AppendPlan:
         self.new_at = [t.data_ptr() for t in self.new_lengths]
         p = self.params = AppendParams()
         self.at, self.call = C.byref(p), binding.load_library().sttm_cache_append
-        self.output = AppendOutput(None, None, self.status)
+        self.output, self.axes = AppendOutput(None, None, self.status), 1 if rotary is None or rotary.sections is None else 3
         p.q_heads, p.eps, p.axes = q_heads, eps, 1
         p.device_status = self.status.data_ptr()
         if rotary is not None:
@@ -174,12 +170,13 @@ class AppendPlan:
             p.q, p.q_row, p.q_head = _heads(q, (rows, self.q_heads, dim), dtype, index, "q")
             if q_out is None:
                 q_out = torch.empty((rows, self.q_heads, dim), dtype=dtype, device=c.device)
-            elif not (_fits(q_out, (rows, self.q_heads, dim), dtype, index) and q_out.is_contiguous()):
+            elif q_out.dtype is not dtype or q_out.shape != q.shape or q_out.get_device() != index or not q_out.is_contiguous():
                 raise ValueError("q_out must be contiguous [rows, q_heads, dim] of the cache's type")
             p.q_out = q_out.data_ptr()
         p.k, p.k_row, p.k_head = _heads(k, (rows, c.heads, dim), dtype, index, "k")
         p.v, p.v_row, p.v_head = _heads(v, (rows, c.heads, dim), dtype, index, "v")
-        if not (_fits(row_offsets, (c.seqs + 1,), torch.int64, index) and row_offsets.is_contiguous()):
+        o = row_offsets
+        if o.dtype is not torch.int64 or o.shape != (c.seqs + 1,) or o.get_device() != index or not o.is_contiguous():
             raise ValueError("row_offsets must be a contiguous int64 tensor [seqs + 1] on the cache's device")
         p.row_offsets, p.rows = row_offsets.data_ptr(), rows
         p.lengths = at = None if lengths is None else _ints(lengths, (c.seqs,), "lengths", index)
@@ -187,13 +184,14 @@ class AppendPlan:
         new = self.new_lengths[which]
         p.new_lengths = self.new_at[which]
         if self.rotary is not None:
-            shape = (rows,) if p.axes == 1 and positions is not None and positions.dim() == 1 else (p.axes, rows)
             floats = positions is not None and positions.dtype is torch.float32
-            if positions is None or not _fits(positions, shape, torch.float32 if floats else torch.int32, index) or (
-                    rows > 1 and positions.stride()[-1] != 1):
+            shape = None if positions is None else positions.shape
+            if (shape is None or not (floats or positions.dtype is torch.int32) or positions.get_device() != index
+                    or shape != (self.axes, rows) and (self.axes > 1 or shape != (rows,)) or rows > 1 and positions.stride()[-1] != 1):
                 raise ValueError("positions must be int32 or float32 [axes, rows] on the cache's device")
             p.positions, p.positions_f32 = positions.data_ptr(), floats
-            p.axis_stride = positions.stride()[0]
+            if self.axes > 1:
+                p.axis_stride = positions.stride()[0]
         if _device() != index:
             c.other_device()
         code = self.call(c.at, self.at, _raw_stream(index))

@@ -149,8 +149,8 @@ struct Share {
 __device__ __forceinline__ int tiles_of(const AttendArgs& p, int len) { return (len + p.tile - 1) / p.tile; }
 __device__ __forceinline__ Share attend_share(const AttendArgs& p, int cta, int lane) {
     Share s;
-    if (p.cluster > 0) {
-        const int row = cta / p.cluster, rank = cta - row * p.cluster, base = row * tiles_of(p, p.max_len);
+    if (p.cluster > 0) {                                    // (the grid is made of clusters, of one CTA at least)
+        const int row = (int)cluster_id(), rank = (int)cluster_rank(), base = row * tiles_of(p, p.max_len);
         s.c.b = row / p.heads;
         s.c.h = row - s.c.b * p.heads;
         s.c.len = attend_length(p, s.c.b);
@@ -277,7 +277,7 @@ __device__ __forceinline__ void attend_leave_nothing(const AttendArgs& p, uint32
 template <typename T, int DIM>
 __device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine, int logits_tile, int tiles) {
     const uint32_t at = smem_u32(mine);
-    const int rank = blockIdx.x % p.cluster, row = blockIdx.x / p.cluster, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank(), row = (int)cluster_id(), lane = threadIdx.x & 31;
     // behind this CTA's part: what every part's outputs count in the end [cluster][group], and the final statistics
     float* factor = reinterpret_cast<float*>(mine + p.group * (DIM * 4 + 8));
     float2* final_stat = reinterpret_cast<float2*>(factor + kAttMaxCluster * p.group);
