@@ -5,7 +5,8 @@
 attention) marshal arguments for sttm_cache_append, sttm_cache_attend and sttm_cache_evict; a plan
 holds buffers and parameters for repeated calls on one cache.  The functions of those names are
 single calls.  All work is enqueued on the current stream, nothing synchronises; conditions found
-on the device are OR-ed into a plan's ``status``, which it never clears.  There is no fallback.
+on the device are OR-ed into a plan's ``status``, which it never clears.  A plan's buffers serve one call after
+the other: use it on one stream, or order the streams.  There is no fallback.
 """
 from __future__ import annotations
 

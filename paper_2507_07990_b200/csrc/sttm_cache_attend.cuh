@@ -72,7 +72,7 @@ struct AttendArgs {
     int4* rows;                   // [seqs * heads] {first tile, first partial, partials, -} (equal shares)
     float2* stats;                // [partials][group] {reference of the exponentials, their sum}
     float* partial;               // [partials][group][DIM]
-    float* logits;                // [tiles][group][64], null without scores
+    float* logits;                // [tiles][group][tile], null without scores
     float* scores;                // may be null
     long long score_seq, score_head;
     float decay;
