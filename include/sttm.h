@@ -322,7 +322,9 @@ typedef struct sttm_cache {
  * Norm, rotation and cache entry of new tokens, one pass.  Row r holds the query, key and value heads
  * of a token; rows row_offsets[b] <= r < row_offsets[b + 1] are sequence b's, in order, and go to its
  * slots lengths[b], lengths[b] + 1, ...  Rows at or beyond row_offsets[seqs] are not touched, so a
- * buffer sized for all tokens of a video can be passed with the offsets that sttm_merge_ex wrote.
+ * buffer sized for all tokens of a video can be passed with the offsets that sttm_merge_ex wrote.  Offsets beyond
+ * `rows` (of a merge whose buffer was too small for its rows) name rows that are not there: new_lengths does not count
+ * them, and 1 << STTM_ERR_CAPACITY is raised.
  *   y = x / sqrt(mean(x^2) + eps) * w        per head of queries and keys, where w is given
  *   (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = position * inv_freq[i]
  * for the pairs (a, b) = channels (i, i + rot / 2), or (2 i, 2 i + 1) when interleaved, i < rot / 2;
@@ -351,7 +353,8 @@ typedef struct sttm_append_params {
     const float *q_norm, *k_norm; /* [dim] weights, NULL: no norm; 16-byte aligned                 */
     float eps;
     int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_CAPACITY (a slot beyond the table: its
-                                     key and value are dropped) and 1 << STTM_ERR_ARG (a page that is not there: dropped) */
+                                     key and value are dropped; offsets beyond the rows) and 1 << STTM_ERR_ARG (a page that
+                                     is not there: dropped) */
 } sttm_append_params;
 sttm_status sttm_cache_append(const sttm_cache* cache, const sttm_append_params* p, void* stream);
 

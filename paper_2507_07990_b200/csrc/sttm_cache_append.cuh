@@ -72,9 +72,14 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_cache_append(const __grid
     let_next_kernel_start();
     const int seqs = a.c.seqs;
     const long long total = a.row_offsets[seqs];
+    // Offsets may name more rows than there are (those of a merge whose output buffer was too small do): a sequence gets
+    // the slots of the rows that are there, no others.
     if (a.new_lengths != nullptr && blockIdx.x == 0)
-        for (int b = threadIdx.x; b < seqs; b += blockDim.x)
-            a.new_lengths[b] = (a.lengths ? a.lengths[b] : 0) + (int)(a.row_offsets[b + 1] - a.row_offsets[b]);
+        for (int b = threadIdx.x; b < seqs; b += blockDim.x) {
+            const long long begin = a.row_offsets[b], end = min(a.row_offsets[b + 1], a.rows);
+            a.new_lengths[b] = (a.lengths ? a.lengths[b] : 0) + (int)max(end - begin, 0ll);
+        }
+    if (total > a.rows && blockIdx.x == 0 && threadIdx.x == 0) raise_status(a.status, kStatusCapacity);
     const long long w = (long long)blockIdx.x * kAppendWarps + warp;
     const long long row = w / a.parts;
     const int part = (int)(w - row * a.parts);

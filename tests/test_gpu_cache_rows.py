@@ -1,0 +1,55 @@
+"""Which rows an append takes, what it says about the others, and how long its outputs stand."""
+import pytest
+import torch
+
+from paper_2507_07990_b200 import binding, cache
+from tests import test_gpu_cache as base
+
+pytestmark = pytest.mark.gpu
+CAPACITY = 1 << 4
+
+
+def offsets(*values):
+    return torch.tensor(values, dtype=torch.int64, device="cuda")
+
+
+@pytest.mark.parametrize("ends,real", [((3, 3, 12), (3, 0, 7)), ((3, 11, 15), (3, 7, 0)), ((10, 10, 11), (10, 0, 0)), ((30, 40, 50), (10, 0, 0))],
+                         ids=str)
+def test_append_counts_only_rows_that_are_there(ends, real):
+    """Offsets may end beyond the rows (a merge whose output buffer was too small counts what it had no room for): the rows
+    that are there are cached, the lengths count no others, and the status says so."""
+    p, want = (base.append_problem(61, rows=(4, 4, 2), held=(0, 2, 20), spare=0, page=32) for _ in range(2))
+    want["offsets"] = offsets(0, real[0], real[0] + real[1], 10)
+    p["offsets"] = offsets(0, *ends)
+    expected, got = base.run_append(want), base.run_append(p)
+    assert got.new_lengths.tolist() == expected.new_lengths.tolist() == [h + r for h, r in zip((0, 2, 20), real)]
+    assert int(got.status) == CAPACITY and int(expected.status) == 0
+    assert torch.equal(got.q, expected.q)
+    for name in ("k_pages", "v_pages"):
+        assert torch.equal(p[name].view(torch.int16), want[name].view(torch.int16))
+
+
+def test_append_of_no_rows_with_offsets_that_name_some():
+    p = base.append_problem(62, rows=(2, 2), held=(5, 7), spare=0)
+    before = p["k_pages"].clone()
+    for name in ("q", "k", "v"):
+        p[name] = p[name][:0]
+    p["pos"] = p["pos"][:, :0]
+    p["offsets"] = offsets(0, 3, 3)
+    out = base.run_append(p)
+    assert out.new_lengths.tolist() == [5, 7] and int(out.status) == CAPACITY
+    assert torch.equal(p["k_pages"].view(torch.int16), before.view(torch.int16))
+
+
+def test_append_of_a_merge_whose_buffer_was_too_small():
+    from paper_2507_07990_b200 import inputs
+    from tests import helpers
+    video = helpers.to_torch(inputs.make_video(helpers.small_spec(61, 6, 13, 13, 64, p_static=0.8)))
+    whole = binding.sttm_merge_ex(video, 0.97, 0.9)
+    n = int(whole.out_count[0])
+    m = binding.sttm_merge_ex(video, 0.97, 0.9, capacity=n - 5)
+    assert int(m.out_offsets[1]) == n and m.out_feats.shape[0] == n - 5
+    pool = cache.empty_cache(1, n, 1, 64)
+    x = m.out_feats.view(-1, 1, 64)
+    out = cache.sttm_cache_append(pool, None, x, x, m.out_offsets)
+    assert out.new_lengths.tolist() == [n - 5] and int(out.status) == CAPACITY
