@@ -321,8 +321,9 @@ typedef struct sttm_cache {
 /*
  * Norm, rotation and cache entry of new tokens, one pass.  Row r holds the query, key and value heads
  * of a token; rows row_offsets[b] <= r < row_offsets[b + 1] are sequence b's, in order, and go to its
- * slots lengths[b], lengths[b] + 1, ...  Rows at or beyond row_offsets[seqs] are not touched, so a
- * buffer sized for all tokens of a video can be passed with the offsets that sttm_merge_ex wrote.  Offsets beyond
+ * slots lengths[b], lengths[b] + 1, ...  Rows before row_offsets[0] and rows at or beyond row_offsets[seqs] are not
+ * touched, so a window into a longer buffer can be passed, and a buffer sized for all tokens of a video with the offsets that
+ * sttm_merge_ex wrote.  Offsets beyond
  * `rows` (of a merge whose buffer was too small for its rows) name rows that are not there: new_lengths does not count
  * them, and 1 << STTM_ERR_CAPACITY is raised.
  *   y = x / sqrt(mean(x^2) + eps) * w        per head of queries and keys, where w is given

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_cache_append(const __grid
     wait_for_prior_kernel();
     let_next_kernel_start();
     const int seqs = a.c.seqs;
-    const long long total = a.row_offsets[seqs];
+    const long long first = a.row_offsets[0], total = a.row_offsets[seqs];      // rows [first, total) are tokens
     // Offsets may name more rows than there are (those of a merge whose output buffer was too small do): a sequence gets
     // the slots of the rows that are there, no others.
     if (a.new_lengths != nullptr && blockIdx.x == 0)
@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) k_cache_append(const __grid
     const long long w = (long long)blockIdx.x * kAppendWarps + warp;
     const long long row = w / a.parts;
     const int part = (int)(w - row * a.parts);
-    if (row >= a.rows || row >= total) return;
+    if (row >= a.rows || row < first || row >= total) return;
 
     const int c = lane % LPH, sub = lane / LPH;
     const int rw = a.rot / 16;                              // rotated words per half = lanes that turn

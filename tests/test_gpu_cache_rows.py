@@ -53,3 +53,27 @@ def test_append_of_a_merge_whose_buffer_was_too_small():
     x = m.out_feats.view(-1, 1, 64)
     out = cache.sttm_cache_append(pool, None, x, x, m.out_offsets)
     assert out.new_lengths.tolist() == [n - 5] and int(out.status) == CAPACITY
+
+
+@pytest.mark.parametrize("first", [1, 2, 9])
+def test_append_leaves_rows_before_the_first_offset_alone(first):
+    """Offsets of a window into a longer buffer: neither the slots in use nor the queries of the rows before it change."""
+    p = base.append_problem(63, rows=(4, 0, 6), held=(12, 3, 30), spare=0)
+    ends = [first, max(first, 4), max(first, 4), 10]
+    p["offsets"] = offsets(*ends)
+    before_k, before_v = p["k_pages"].clone(), p["v_pages"].clone()
+    q_out = torch.full_like(p["q"].contiguous(), 7.0)
+    out = base.run_append(p, q_out)
+    assert torch.equal(q_out[:first], torch.full_like(q_out[:first], 7.0)) and not (q_out[first:] == 7.0).all()
+    rows = [b - a for a, b in zip(ends, ends[1:])]
+    assert out.new_lengths.tolist() == [h + r for h, r in zip((12, 3, 30), rows)] and int(out.status) == 0
+    touched = torch.zeros(before_k.shape[0], 16, dtype=torch.bool)
+    for b, (h, r) in enumerate(zip((12, 3, 30), rows)):
+        for i in range(r):
+            pg, place = int(p["table"][b, (h + i) // 16]), (h + i) % 16
+            touched[pg, place] = True
+            assert torch.equal(p["v_pages"][pg, :, place], p["v"][ends[b] + i])
+    touched = touched.cuda()
+    for now, was in ((p["k_pages"], before_k), (p["v_pages"], before_v)):
+        same = (now.view(torch.int16) == was.view(torch.int16)).all(3).all(1)
+        assert same[~touched].all()
