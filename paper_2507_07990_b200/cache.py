@@ -133,14 +133,14 @@ class AppendPlan:
     def __init__(self, cache: PagedCache, q_heads: int, rotary: Optional[Rotary] = None, q_norm: Optional[torch.Tensor] = None,
                  k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
         self.cache, self.q_heads, self.rotary, self.keep = cache, q_heads, rotary, (q_norm, k_norm)
-        # two of them: the lengths that a call reads may be those that the call before it wrote
+        # three of them: a call writes neither what the call before it wrote nor what it reads
         n = cache.seqs
-        ints = torch.zeros(2 * n + 1, dtype=torch.int32, device=cache.device)
-        self.new_lengths, self.status = [ints[:n], ints[n:2 * n]], ints[2 * n:]
-        self.new_at = [t.data_ptr() for t in self.new_lengths]
+        ints = torch.zeros(3 * n + 1, dtype=torch.int32, device=cache.device)
+        self.new_lengths, self.status = [ints[i * n:(i + 1) * n] for i in range(3)], ints[3 * n:]
+        self.new_at, self.written = [t.data_ptr() for t in self.new_lengths], 2
         p = self.params = AppendParams()
         self.at, self.call = C.byref(p), binding.load_library().sttm_cache_append
-        self.output, self.axes = AppendOutput(None, None, self.status), 1 if rotary is None or rotary.sections is None else 3
+        self.axes = 1 if rotary is None or rotary.sections is None else 3
         p.q_heads, p.eps, p.axes = q_heads, eps, 1
         p.device_status = self.status.data_ptr()
         if rotary is not None:
@@ -163,8 +163,8 @@ class AppendPlan:
             q_out: Optional[torch.Tensor] = None) -> AppendOutput:
         """``q`` ``[rows, q_heads, dim]``, ``k``, ``v`` ``[rows, heads, dim]`` (any row and head strides, views of one
         projection for instance); ``row_offsets`` int64 ``[seqs + 1]``; ``lengths`` int32 ``[seqs]`` (None: an empty cache);
-        ``positions`` int32 or float32 ``[rows]`` or ``[axes, rows]``.  The plan returns the same object every time;
-        the ``new_lengths`` tensor it names is written again by the call after the next."""
+        ``positions`` int32 or float32 ``[rows]`` or ``[axes, rows]``.  The ``new_lengths`` that it returns stand until the call after
+        the next, whatever lengths either is given."""
         c, p = self.cache, self.params
         dim, dtype, index, rows = c.dim, c.dtype, c.index, k.shape[0]
         if self.q_heads > 0:
@@ -181,8 +181,9 @@ class AppendPlan:
             raise ValueError("row_offsets must be a contiguous int64 tensor [seqs + 1] on the cache's device")
         p.row_offsets, p.rows = row_offsets.data_ptr(), rows
         p.lengths = at = None if lengths is None else _ints(lengths, (c.seqs,), "lengths", index)
-        which = 1 if at == self.new_at[0] else 0
-        new = self.new_lengths[which]
+        which = (self.written + 1) % 3
+        if at == self.new_at[which]:
+            which = (which + 1) % 3
         p.new_lengths = self.new_at[which]
         if self.rotary is not None:
             floats = positions is not None and positions.dtype is torch.float32
@@ -198,9 +199,8 @@ class AppendPlan:
         code = self.call(c.at, self.at, _raw_stream(index))
         if code:
             _check(code, "sttm_cache_append")
-        out = self.output
-        out.q, out.new_lengths = q_out, new
-        return out
+        self.written = which
+        return AppendOutput(q_out, self.new_lengths[which], self.status)
 
 
 @dataclass

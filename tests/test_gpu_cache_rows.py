@@ -77,3 +77,31 @@ def test_append_leaves_rows_before_the_first_offset_alone(first):
     for now, was in ((p["k_pages"], before_k), (p["v_pages"], before_v)):
         same = (now.view(torch.int16) == was.view(torch.int16)).all(3).all(1)
         assert same[~touched].all()
+
+
+def test_append_lengths_outlive_the_next_call():
+    """A call's new lengths are written again by the call after the next, whatever lengths either is given."""
+    p = base.append_problem(64, rows=(1, 1), held=(3, 9), spare=0, page=32)
+    plan = cache.AppendPlan(cache.PagedCache(p["k_pages"], p["v_pages"], p["table"]), 4, cache.Rotary(p["freq"]))
+    step = lambda lengths: plan.run(p["q"], p["k"], p["v"], p["offsets"], lengths, p["pos"])
+    older, latest = step(p["lengths"]).new_lengths, step(None).new_lengths
+    # a caller's lengths, none, the plan's latest, the plan's latest but one: every order of two of them
+    for kind in "ccnnclpnplcplnlppccpnncl":
+        lengths = {"c": p["lengths"], "n": None, "l": latest, "p": older}[kind]
+        given, was = [0, 0] if lengths is None else lengths.tolist(), latest.tolist()
+        new = step(lengths).new_lengths
+        assert new.tolist() == [n + 1 for n in given], kind
+        assert latest.tolist() == was, kind
+        assert lengths is None or lengths.tolist() == given, kind
+        older, latest = latest, new
+    assert int(plan.status) == 0
+
+
+def test_append_outputs_of_two_calls_are_two_objects():
+    p = base.append_problem(65, rows=(1,), held=(3,), spare=0)
+    plan = cache.AppendPlan(cache.PagedCache(p["k_pages"], p["v_pages"], p["table"]), 4, cache.Rotary(p["freq"]))
+    first = plan.run(p["q"], p["k"], p["v"], p["offsets"], p["lengths"], p["pos"])
+    q, new = first.q, first.new_lengths
+    second = plan.run(p["q"], p["k"], p["v"], p["offsets"], first.new_lengths, p["pos"])
+    assert first.q is q and first.new_lengths is new and second.new_lengths is not new
+    assert first.new_lengths.tolist() == [4] and second.new_lengths.tolist() == [5]
