@@ -122,6 +122,8 @@ struct AttendPlan {
     int cluster;                  // see AttendArgs
     long long tiles;              // upper bound over all rows
     int row_tiles, grid_limit;
+    long long join_blocks, join_grid;   // k_cache_join's blocks that join rows, and all
+    int chunks;                   // blocks per row that update scores
     size_t rows, stats, partial, logits, total;
 };
 
@@ -145,6 +147,12 @@ sttm_status plan_attend(const sttm_cache* c, const sttm_attend_params* p, Attend
     while (size < most && size < pl->row_tiles && rows * size * 2 <= sm_count()) size *= 2;
     const bool many = rows * 2 > pl->grid_limit;
     pl->cluster = pl->row_tiles <= size * (many ? kWholeTiles : kClusterTiles) && (many || p->scores == nullptr) ? size : 0;
+    // blocks per row that update scores: one go each while all of them are resident at once
+    pl->join_blocks = rows * group;
+    pl->chunks = (int)std::min<long long>(((long long)p->max_len + kScoreSlots - 1) / kScoreSlots,
+                                          std::max<long long>(1, (long long)sm_count() * 8 / rows));
+    pl->join_grid = pl->join_blocks + (p->scores ? rows * pl->chunks : 0);
+    if (!pl->cluster && pl->join_grid > INT_MAX) return STTM_ERR_UNSUPPORTED;       // (before the first kernel runs)
     const long long parts = pl->cluster ? (pl->cluster == 1 ? rows : 0) : std::min<long long>(pl->grid_limit, pl->tiles) + rows;
     pl->rows = 0;
     pl->stats = align_up((size_t)rows * sizeof(int4));
@@ -283,7 +291,6 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
     CUtensorMap mk, mv;
     if ((s = make_cache_map(cache, cache->k, a.box, &mk)) != STTM_OK) return s;
     if ((s = make_cache_map(cache, cache->v, a.box, &mv)) != STTM_OK) return s;
-    const long long rows = (long long)a.seqs * a.heads;
     return by_type(cache, [&](auto tag, auto dim) {
         using T = decltype(tag);
         constexpr int D = decltype(dim)::value;
@@ -291,12 +298,7 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
         a.stages = D == 256 ? 6 : 3;
         sttm_status r = a.group <= 8 ? launch_attend<T, D, 8>(a, pl, mk, mv, stream) : launch_attend<T, D, 16>(a, pl, mk, mv, stream);
         if (r != STTM_OK || pl.cluster) return r;
-        const long long join_blocks = rows * a.group;
-        // blocks per row that update scores: one go each while all of them are resident at once
-        const int chunks = (int)std::min<long long>((p->max_len + kScoreSlots - 1) / kScoreSlots,
-                                                    std::max<long long>(1, (long long)sm_count() * 8 / rows));
-        const long long grid = join_blocks + (p->scores ? rows * chunks : 0);
-        return launch(k_cache_join<T, D>, grid, kJoinThreads, 0, 0, stream, a, (int)join_blocks, chunks);
+        return launch(k_cache_join<T, D>, pl.join_grid, kJoinThreads, 0, 0, stream, a, (int)pl.join_blocks, pl.chunks);
     });
 }
 
