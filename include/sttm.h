@@ -374,7 +374,7 @@ typedef struct sttm_attend_params {
     int q_heads;                  /* a multiple of the cache's heads, at most 64 per KV head       */
     const int32_t* lengths;       /* [seqs] slots in use (the new token's own among them)          */
     int max_len;                  /* no length is larger (else it is cut and 1 << STTM_ERR_CAPACITY raised); at most
-                                     table_width * page */
+                                     table_width * page, and below 2^31 - 2^20                     */
     float scale;
     const uint8_t* mask;          /* [seqs][mask_stride], mask_stride >= max_len, or NULL          */
     long long mask_stride;
@@ -407,7 +407,7 @@ typedef struct sttm_evict_params {
     int first, last;              /* protected slots                                               */
     const float* scores;          /* [seqs][heads][max_len]                                        */
     long long score_seq, score_head;   /* strides in elements                                      */
-    int kept_width;               /* columns of kept and new_scores                                */
+    int kept_width;               /* columns of kept and new_scores, below 2^31 - 2^20             */
     int32_t* new_lengths;         /* [seqs] out                                                    */
     int32_t* kept;                /* [seqs][heads][kept_width] out: the slots kept, then -1        */
     float* new_scores;            /* [seqs][heads][kept_width] out: their scores, then 0           */

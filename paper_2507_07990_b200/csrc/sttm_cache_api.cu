@@ -49,6 +49,10 @@ sttm_status allow_smem(const void* kernel, size_t bytes, size_t (&allowed)[kMaxD
     return STTM_OK;
 }
 
+// Slots of a row at most: the kernels count them in 32 bits and step up to sm_count() * 4096 beyond the last
+// (148 multiprocessors: 606208).
+constexpr int kMaxSlots = INT_MAX - (1 << 20);
+
 bool multiple_of_8(long long v) { return v % 8 == 0; }
 
 sttm_status check_cache(const sttm_cache* c) {
@@ -133,7 +137,7 @@ sttm_status plan_attend(const sttm_cache* c, const sttm_attend_params* p, Attend
     if (p == nullptr || p->q_heads < 1 || p->q_heads % c->heads != 0 || p->max_len < 1) return STTM_ERR_ARG;
     if ((long long)p->max_len > (long long)c->table_width * c->page) return STTM_ERR_ARG;
     const int group = p->q_heads / c->heads;
-    if (group > 64) return STTM_ERR_UNSUPPORTED;
+    if (group > 64 || p->max_len > kMaxSlots) return STTM_ERR_UNSUPPORTED;
     const long long rows = (long long)c->seqs * c->heads;
     const int tile = attend_tile(c->dim);
     pl->row_tiles = (p->max_len + tile - 1) / tile;
@@ -149,7 +153,7 @@ sttm_status plan_attend(const sttm_cache* c, const sttm_attend_params* p, Attend
     pl->cluster = pl->row_tiles <= size * (many ? kWholeTiles : kClusterTiles) && (many || p->scores == nullptr) ? size : 0;
     // blocks per row that update scores: one go each while all of them are resident at once
     pl->join_blocks = rows * group;
-    pl->chunks = (int)std::min<long long>(((long long)p->max_len + kScoreSlots - 1) / kScoreSlots,
+    pl->chunks = (int)std::min<long long>((p->max_len + kScoreSlots - 1) / kScoreSlots,
                                           std::max<long long>(1, (long long)sm_count() * 8 / rows));
     pl->join_grid = pl->join_blocks + (p->scores ? rows * pl->chunks : 0);
     if (!pl->cluster && pl->join_grid > INT_MAX) return STTM_ERR_UNSUPPORTED;       // (before the first kernel runs)
@@ -312,6 +316,7 @@ sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const
     if (src->heads != dst->heads || src->dim != dst->dim || src->dtype != dst->dtype || src->seqs != dst->seqs) return STTM_ERR_ARG;
     if (p->max_len < 1 || (long long)p->max_len > (long long)src->table_width * src->page || p->kept_width < 1) return STTM_ERR_ARG;
     if (p->first < 0 || p->last < 0) return STTM_ERR_ARG;
+    if (p->max_len > kMaxSlots || p->kept_width > kMaxSlots) return STTM_ERR_UNSUPPORTED;
     if (p->new_lengths == p->lengths || p->new_lengths == p->keep || p->new_scores == p->scores) return STTM_ERR_ARG;
     EvictArgs a = {};
     a.src = view_of(src);

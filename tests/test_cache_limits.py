@@ -2,7 +2,24 @@
 import ctypes as C
 
 from paper_2507_07990_b200 import binding
-from tests.test_cache_refusals import AT, UNSUPPORTED, attend, pool
+from tests.test_cache_refusals import AT, UNSUPPORTED, attend, evict, pool
+
+WIDTH = (2 ** 31 - 1) // 8              # pages of 8 slots: the longest table there is
+
+
+def test_lengths_whose_slots_cannot_be_counted_in_steps():
+    """The kernels step over a row's slots in 32-bit integers, up to 606208 at a time."""
+    lib = binding.load_library()
+    c = pool(page=8, table_width=WIDTH, table_stride=WIDTH, heads=1, seqs=1)
+    for n in (8 * WIDTH, 2 ** 31 - 2 ** 20):
+        for kw in (dict(), dict(scores=AT), dict(mask=AT, mask_stride=n)):
+            p = attend(max_len=n, q_heads=1, **kw)
+            assert lib.sttm_attend_workspace_bytes(C.byref(c), C.byref(p)) == 0, (n, kw)
+            assert lib.sttm_cache_attend(C.byref(c), C.byref(p), AT, 1 << 60, None) == UNSUPPORTED, (n, kw)
+        assert lib.sttm_cache_evict(C.byref(c), C.byref(pool(heads=1, seqs=1)), C.byref(evict(max_len=n)), None) == UNSUPPORTED, n
+        assert lib.sttm_cache_evict(C.byref(pool()), C.byref(pool()), C.byref(evict(kept_width=n)), None) == UNSUPPORTED, n
+    # (bytes of a workspace, no call) the longest that is taken
+    assert lib.sttm_attend_workspace_bytes(C.byref(c), C.byref(attend(max_len=2 ** 31 - 2 ** 20 - 1, q_heads=1))) > 0
 
 
 def test_a_grid_that_only_the_second_launch_could_not_have():
