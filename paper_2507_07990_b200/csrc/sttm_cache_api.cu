@@ -54,6 +54,9 @@ sttm_status allow_smem(const void* kernel, size_t bytes, size_t (&allowed)[kMaxD
 constexpr int kMaxSlots = INT_MAX - (1 << 20);
 
 bool multiple_of_8(long long v) { return v % 8 == 0; }
+// is any of these arrays of 4-byte numbers (or NULL) at an address that is no multiple of 4?
+template <typename... P>
+bool odd_address(const P*... p) { return (((uintptr_t)p | ...) & 3) != 0; }
 
 sttm_status check_cache(const sttm_cache* c) {
     if (c == nullptr || c->k == nullptr || c->v == nullptr || c->table == nullptr) return STTM_ERR_ARG;
@@ -62,7 +65,7 @@ sttm_status check_cache(const sttm_cache* c) {
     if (c->dim != 64 && c->dim != 128 && c->dim != 256) return STTM_ERR_UNSUPPORTED;
     if (c->page % 8 != 0 || c->pages > INT_MAX - 1) return STTM_ERR_UNSUPPORTED;
     if ((long long)c->table_width * c->page > INT_MAX || (long long)c->seqs * c->heads > INT_MAX / 64) return STTM_ERR_UNSUPPORTED;
-    if (misaligned(c->k, 16) || misaligned(c->v, 16)) return STTM_ERR_ARG;
+    if (misaligned(c->k, 16) || misaligned(c->v, 16) || odd_address(c->table)) return STTM_ERR_ARG;
     // (the stride of an axis of length one is never used)
     if ((c->pages > 1 && !multiple_of_8(c->page_stride)) || (c->heads > 1 && !multiple_of_8(c->head_stride)) || !multiple_of_8(c->slot_stride))
         return STTM_ERR_ARG;
@@ -192,6 +195,8 @@ sttm_status sttm_cache_append(const sttm_cache* cache, const sttm_append_params*
     if (s != STTM_OK) return s;
     if (p == nullptr || p->row_offsets == nullptr || p->rows < 0 || p->q_heads < 0) return STTM_ERR_ARG;
     if (p->new_lengths != nullptr && p->new_lengths == p->lengths) return STTM_ERR_ARG;
+    if (misaligned(p->row_offsets, 8) || odd_address(p->lengths, p->new_lengths, p->inv_freq, p->device_status, (const int32_t*)p->positions))
+        return STTM_ERR_ARG;
     if (p->rot < 0 || p->rot > cache->dim || p->rot % 16 != 0) return STTM_ERR_ARG;
     if (p->rows > 0) {
         if (p->k == nullptr || p->v == nullptr || (p->q_heads > 0 && (p->q == nullptr || p->q_out == nullptr))) return STTM_ERR_ARG;
@@ -257,6 +262,7 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
     if (s != STTM_OK) return s;
     if (p->q == nullptr || p->out == nullptr || p->lengths == nullptr || ws == nullptr) return STTM_ERR_ARG;
     if (misaligned(p->q, 16) || misaligned(p->out, 16) || misaligned(ws, 256)) return STTM_ERR_ARG;
+    if (odd_address(p->lengths, p->scores, p->lse, p->device_status)) return STTM_ERR_ARG;
     if (!multiple_of_8(p->q_seq) || !multiple_of_8(p->q_head) || !std::isfinite(p->scale)) return STTM_ERR_ARG;
     if (p->mask != nullptr && cache->seqs > 1 && p->mask_stride < p->max_len) return STTM_ERR_ARG;
     if (ws_bytes < pl.total) return STTM_ERR_WORKSPACE;
@@ -317,6 +323,7 @@ sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const
     if (p->max_len < 1 || (long long)p->max_len > (long long)src->table_width * src->page || p->kept_width < 1) return STTM_ERR_ARG;
     if (p->first < 0 || p->last < 0) return STTM_ERR_ARG;
     if (p->max_len > kMaxSlots || p->kept_width > kMaxSlots) return STTM_ERR_UNSUPPORTED;
+    if (odd_address(p->lengths, p->keep, p->scores, p->new_lengths, p->kept, p->new_scores, p->device_status)) return STTM_ERR_ARG;
     if (p->new_lengths == p->lengths || p->new_lengths == p->keep || p->new_scores == p->scores) return STTM_ERR_ARG;
     EvictArgs a = {};
     a.src = view_of(src);

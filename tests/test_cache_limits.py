@@ -2,7 +2,7 @@
 import ctypes as C
 
 from paper_2507_07990_b200 import binding
-from tests.test_cache_refusals import AT, UNSUPPORTED, attend, evict, pool
+from tests.test_cache_refusals import ARG, AT, UNSUPPORTED, append, attend, evict, pool
 
 WIDTH = (2 ** 31 - 1) // 8              # pages of 8 slots: the longest table there is
 
@@ -31,3 +31,22 @@ def test_a_grid_that_only_the_second_launch_could_not_have():
     assert lib.sttm_attend_workspace_bytes(C.byref(c), C.byref(plain)) > 0
     assert lib.sttm_attend_workspace_bytes(C.byref(c), C.byref(scored)) == 0
     assert lib.sttm_cache_attend(C.byref(c), C.byref(scored), AT, 1 << 60, None) == UNSUPPORTED
+
+
+def test_arrays_of_numbers_at_odd_addresses():
+    """A kernel that read them there would end with a misaligned address."""
+    lib = binding.load_library()
+    for table in (AT + 2, AT + 1):
+        bad = pool(table=table)
+        assert lib.sttm_cache_attend(C.byref(bad), C.byref(attend()), AT, 1 << 30, None) == ARG
+        assert lib.sttm_cache_append(C.byref(bad), C.byref(append()), None) == ARG
+        assert lib.sttm_cache_evict(C.byref(pool()), C.byref(bad), C.byref(evict()), None) == ARG
+    for off in (1, 2, 3):
+        at = AT + 2048 + off
+        for kw in [dict(lengths=at), dict(lse=at), dict(device_status=at), dict(scores=at, score_seq=256, score_head=64)]:
+            assert lib.sttm_cache_attend(C.byref(pool()), C.byref(attend(**kw)), AT, 1 << 30, None) == ARG, kw
+        for kw in [dict(lengths=at), dict(new_lengths=at), dict(positions=at), dict(inv_freq=at), dict(device_status=at), dict(row_offsets=at),
+                   dict(row_offsets=AT + 4)]:
+            assert lib.sttm_cache_append(C.byref(pool()), C.byref(append(**kw)), None) == ARG, kw
+        for kw in [dict(lengths=at), dict(keep=at), dict(scores=at), dict(new_lengths=at), dict(kept=at), dict(new_scores=at), dict(device_status=at)]:
+            assert lib.sttm_cache_evict(C.byref(pool()), C.byref(pool()), C.byref(evict(**kw)), None) == ARG, kw
