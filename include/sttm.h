@@ -379,7 +379,8 @@ typedef struct sttm_attend_params {
     const uint8_t* mask;          /* [seqs][mask_stride], mask_stride >= max_len, or NULL          */
     long long mask_stride;
     float* scores;                /* in and out, or NULL                                           */
-    long long score_seq, score_head;   /* strides in elements, from one sequence / KV head to the next */
+    long long score_seq, score_head;   /* strides in elements, from one sequence / KV head to the next: either axis inside the
+                                     other's stride, no two rows of max_len in the same memory     */
     float decay;
     void* out;                    /* [seqs][q_heads][dim] contiguous                               */
     float* lse;                   /* [seqs][q_heads] log of the sum of exp(scale q . k), may be NULL */

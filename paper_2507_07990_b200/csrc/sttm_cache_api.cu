@@ -58,6 +58,15 @@ bool multiple_of_8(long long v) { return v % 8 == 0; }
 template <typename... P>
 bool odd_address(const P*... p) { return (((uintptr_t)p | ...) & 3) != 0; }
 
+// Do rows of `len` numbers, `seq` elements from one sequence to the next and `head` from one of its heads to the next, share any?
+// (One axis has to lie inside the other's stride; the stride of an axis of length one says nothing.)
+bool rows_overlap(long long seq, long long head, int seqs, int heads, int len) {
+    if (seqs == 1 && heads == 1) return false;
+    if (seqs == 1 || heads == 1) return (heads == 1 ? seq : head) < len;
+    const long long inner = std::min(seq, head), outer = std::max(seq, head), last = (seq < head ? seqs : heads) - 1;
+    return inner < len || outer < len || (outer - len) / last < inner;
+}
+
 sttm_status check_cache(const sttm_cache* c) {
     if (c == nullptr || c->k == nullptr || c->v == nullptr || c->table == nullptr) return STTM_ERR_ARG;
     if (c->pages < 1 || c->heads < 1 || c->page < 1 || c->seqs < 1 || c->table_width < 1 || c->dim < 1) return STTM_ERR_ARG;
@@ -263,6 +272,7 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
     if (p->q == nullptr || p->out == nullptr || p->lengths == nullptr || ws == nullptr) return STTM_ERR_ARG;
     if (misaligned(p->q, 16) || misaligned(p->out, 16) || misaligned(ws, 256)) return STTM_ERR_ARG;
     if (odd_address(p->lengths, p->scores, p->lse, p->device_status)) return STTM_ERR_ARG;
+    if (p->scores != nullptr && rows_overlap(p->score_seq, p->score_head, cache->seqs, cache->heads, p->max_len)) return STTM_ERR_ARG;
     if (!multiple_of_8(p->q_seq) || !multiple_of_8(p->q_head) || !std::isfinite(p->scale)) return STTM_ERR_ARG;
     if (p->mask != nullptr && cache->seqs > 1 && p->mask_stride < p->max_len) return STTM_ERR_ARG;
     if (ws_bytes < pl.total) return STTM_ERR_WORKSPACE;

@@ -50,3 +50,21 @@ def test_arrays_of_numbers_at_odd_addresses():
             assert lib.sttm_cache_append(C.byref(pool()), C.byref(append(**kw)), None) == ARG, kw
         for kw in [dict(lengths=at), dict(keep=at), dict(scores=at), dict(new_lengths=at), dict(kept=at), dict(new_scores=at), dict(device_status=at)]:
             assert lib.sttm_cache_evict(C.byref(pool()), C.byref(pool()), C.byref(evict(**kw)), None) == ARG, kw
+
+
+def test_scores_whose_rows_overlap_cannot_be_updated():
+    """Every row of scores is read and written by a call; rows that share memory would be updated in any order."""
+    lib = binding.load_library()
+    need = lib.sttm_attend_workspace_bytes(C.byref(pool()), C.byref(attend(scores=AT, score_seq=128, score_head=64)))
+    assert need > 0
+    # (3 sequences, 2 heads, 64 slots)
+    for seq, head in ((0, 64), (128, 0), (128, 63), (64, 64), (127, 64), (64, 191), (64, 64 * 2), (-128, 64), (128, -64)):
+        p = attend(scores=AT, score_seq=seq, score_head=head)
+        assert lib.sttm_cache_attend(C.byref(pool()), C.byref(p), AT, 1 << 30, None) == ARG, (seq, head)
+    # either axis may lie inside the other, and the stride of an axis of length one says nothing: these get as far as the workspace
+    for seqs, heads, seq, head in ((3, 2, 128, 64), (3, 2, 200, 70), (3, 2, 64, 192), (1, 2, 0, 64), (3, 1, 64, 0), (1, 1, 0, 0)):
+        c = pool(seqs=seqs, heads=heads)
+        p = attend(scores=AT, score_seq=seq, score_head=head)
+        assert lib.sttm_cache_attend(C.byref(c), C.byref(p), AT, 0, None) == 3, (seqs, heads, seq, head)
+    # an eviction only reads them: one row of scores may serve all sequences and heads (this one is refused for its widths alone)
+    assert lib.sttm_cache_evict(C.byref(pool()), C.byref(pool()), C.byref(evict(score_seq=0, score_head=0, kept_width=0)), None) == ARG
