@@ -243,11 +243,11 @@ __device__ __forceinline__ void attend_empty(const AttendArgs& p, int row) {
 __device__ __forceinline__ float2 weight_of(float ref, float sum) {
     return make_float2(ref == -INFINITY ? 0.f : ref, sum == 0.f ? 0.f : 1.f / sum);
 }
-// slots [from, to) of a row: every slot's weights, added up over the query heads, go to its score
-__device__ __forceinline__ void add_scores(const AttendArgs& p, int b, int h, int from, int to, int first_tile, const float2* stat,
-                                           int thread, int threads) {
+// slots [0, len) of a row: every slot's weights, added up over the query heads, go to its score
+__device__ __forceinline__ void add_scores(const AttendArgs& p, int b, int h, int len, int first_tile, const float2* stat, int thread,
+                                           int threads) {
     float* score = p.scores + b * p.score_seq + h * p.score_head;
-    for (int i = from + thread; i < to; i += threads) {
+    for (int i = thread; i < len; i += threads) {
         const float* x = p.logits + ((long long)(first_tile + i / p.tile) * p.group) * p.tile + i % p.tile;
         const float before = score[i];
         float w = 0.f;
@@ -266,8 +266,8 @@ __device__ __forceinline__ void add_scores(const AttendArgs& p, int b, int h, in
 }
 
 // ---- joining the CTAs of a cluster that share a row.  Every CTA leaves its part in its own shared memory:
-// [group][DIM] outputs, then {reference, sum} per head; after a cluster barrier each takes its share of the outputs, and
-// its own slots' scores.
+// [group][DIM] outputs, then {reference, sum} per head; after a cluster barrier each takes its share of the outputs.
+// (Calls with scores have no clusters of more than one CTA.)
 template <int DIM>
 __device__ __forceinline__ void attend_leave_nothing(const AttendArgs& p, uint32_t at) {
     for (int i = threadIdx.x; i < p.group * DIM / 2; i += kAttWarps * 32) sts_f32x2(at + i * 8, 0.f, 0.f);
@@ -275,12 +275,11 @@ __device__ __forceinline__ void attend_leave_nothing(const AttendArgs& p, uint32
 }
 // by all threads of all CTAs of the cluster
 template <typename T, int DIM>
-__device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine, int logits_tile, int tiles) {
+__device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine) {
     const uint32_t at = smem_u32(mine);
     const int rank = (int)cluster_rank(), row = (int)cluster_id(), lane = threadIdx.x & 31;
-    // behind this CTA's part: what every part's outputs count in the end [cluster][group], and the final statistics
+    // behind this CTA's part: what every part's outputs count in the end [cluster][group]
     float* factor = reinterpret_cast<float*>(mine + p.group * (DIM * 4 + 8));
-    float2* final_stat = reinterpret_cast<float2*>(factor + kAttMaxCluster * p.group);
     cluster_arrive();
     cluster_wait();
     // this CTA's share of the channel pairs: the first of them (as a rule all) are asked for with the statistics
@@ -306,10 +305,7 @@ __device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (is) factor[r * p.group + h] = sum == 0.f ? 0.f : f / sum;
-        if (is && r == 0) {
-            final_stat[h] = weight_of(ref, sum);
-            if (rank == 0 && p.lse != nullptr) p.lse[(long long)row * p.group + h] = (ref + log2f(sum)) * kLn2;
-        }
+        if (is && r == 0 && rank == 0 && p.lse != nullptr) p.lse[(long long)row * p.group + h] = (ref + log2f(sum)) * kLn2;
     }
     __syncthreads();
     for (; i < end; i += kAttThreads) {
@@ -324,12 +320,6 @@ __device__ __noinline__ void attend_join_cluster(const AttendArgs& p, char* mine
             }
         reinterpret_cast<uint32_t*>(p.out)[(long long)row * pairs + i] = Pair<T>::pack(x, y);
         if (i + kAttThreads < end) ask(i + kAttThreads);
-    }
-    if (p.logits != nullptr && tiles > 0) {
-        const int first_tile = logits_tile - row * tiles_of(p, p.max_len);      // of this CTA in the row
-        const int b = row / p.heads, from = first_tile * p.tile;
-        add_scores(p, b, row % p.heads, from, min(attend_length(p, b), from + tiles * p.tile), logits_tile - first_tile, final_stat, threadIdx.x,
-                   kAttThreads);
     }
     cluster_arrive();
     cluster_wait();                                         // nobody leaves while its part may be read
@@ -500,7 +490,7 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
             }
         }
         if (timed_out && lane == 0) raise_status(p.status, kStatusWaitTimeout);
-        if (p.cluster > 1) attend_join_cluster<T, DIM>(p, ring_ptr, t0, t1 - t0);
+        if (p.cluster > 1) attend_join_cluster<T, DIM>(p, ring_ptr);
         return;
     }
 
@@ -799,7 +789,7 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
                         final_stat[h] = weight_of(v.x, v.y);
                     }
                     named_sync(1, kAttWarps * 32);
-                    add_scores(p, c.b, c.h, 0, c.len, first, final_stat, threadIdx.x, kAttWarps * 32);
+                    add_scores(p, c.b, c.h, c.len, first, final_stat, threadIdx.x, kAttWarps * 32);
                 }
             }
         }
@@ -820,7 +810,7 @@ k_cache_attend(const __grid_constant__ AttendArgs p, const __grid_constant__ CUt
             if (p.lengths[b] < 0 || p.lengths[b] > p.max_len) raise_status(p.status, kStatusCapacity);
     if (p.cluster > 1) {
         if (t0 >= t1) attend_leave_nothing<DIM>(p, ring);
-        attend_join_cluster<T, DIM>(p, ring_ptr, t0, t1 - t0);
+        attend_join_cluster<T, DIM>(p, ring_ptr);
     }
 }
 
