@@ -13,7 +13,7 @@ attention; norms of queries and keys, rotation, cache entry, cached attention an
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Optional
+from typing import Iterable, List, Optional
 
 import torch
 import torch.nn.functional as F
@@ -38,6 +38,14 @@ class Config:
 def _rms(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     y = x.float()
     return (y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6) * w).to(x.dtype)
+
+
+def _check_status(name: str, statuses: Iterable[torch.Tensor]) -> None:
+    """Raises what any call has written into its status (waits for the calls)."""
+    bits = 0
+    for word in torch.cat(list(statuses)).tolist():
+        bits |= word
+    binding._check(binding.load_library().sttm_status_from_bits(bits), name)
 
 
 class Answerer:
@@ -68,7 +76,8 @@ class Answerer:
         return cache.AppendPlan(pool, self.cfg.q_heads, self.rotary, q_norm=layer["q_norm"], k_norm=layer["k_norm"])
 
     def watch(self, video: torch.Tensor, tau_s: float, tau_t: float) -> int:
-        """Merges one video ``[T, H, W, width]`` and caches its rows; returns their number."""
+        """Merges one video ``[T, H, W, width]`` and caches its rows; returns their number.  What a call reports in its status
+        is raised (SttmError), here and in ``ask``."""
         c = self.cfg
         T, H, W, _ = video.shape
         merged = binding.sttm_merge_ex(video, tau_s, tau_t, out_dtype=c.dtype)
@@ -78,16 +87,19 @@ class Answerer:
         x, positions = merged.out_feats[:n], merged.out_pos[:n]
         offsets = torch.tensor([0, n], device=self.device)
         self.pools: List[cache.PagedCache] = []
-        self.tails = []
+        statuses = [merged.device_status]
         for layer in self.layers:
             pool = cache.empty_cache(1, n, c.kv_heads, c.dim, c.page, c.dtype, self.device)
             q, k, v = self._qkv(layer, x)
-            q = self._append_plan(pool, layer).run(q, k, v, offsets, None, positions).q
+            entered = self._append_plan(pool, layer).run(q, k, v, offsets, None, positions)
+            q = entered.q
             self.pools.append(pool)
+            statuses.append(entered.status)
             # the video's own attention, from the cache's keys and values in slot order
             ks, vs = (t.transpose(1, 2).reshape(-1, c.kv_heads, c.dim)[:n].transpose(0, 1).unsqueeze(0) for t in (pool.k, pool.v))
             att = F.scaled_dot_product_attention(q.transpose(0, 1).unsqueeze(0), ks, vs, is_causal=True, enable_gqa=True)
             x = self._rest(layer, x, att[0].transpose(0, 1))
+        _check_status("Answerer.watch", statuses)
         return n
 
     def _question_caches(self, questions: int, more: int) -> List[cache.PagedCache]:
@@ -126,6 +138,10 @@ class Answerer:
                     attend=[cache.AttendPlan(p, self.cfg.q_heads) for p in pools],
                     scores=[torch.zeros((questions, p.heads, slots), device=self.device) for p in pools] if scored else None)
 
+    @staticmethod
+    def _statuses(state: dict) -> List[torch.Tensor]:
+        return [plan.status for plan in state["append"] + state["attend"]]
+
     def ask(self, questions: torch.Tensor, answer_tokens: int, keep: Optional[int] = None) -> torch.Tensor:
         """``questions`` ``[questions, length]`` token ids; ``keep``: slots that every cache keeps when the questions have
         been read (None: all).  Returns greedy answers ``[questions, answer_tokens]``."""
@@ -133,6 +149,7 @@ class Answerer:
         pools = self._question_caches(n, length + answer_tokens)
         lengths = torch.full((n,), self.rows, dtype=torch.int32, device=self.device)
         state = self._state(pools, lengths, keep is not None)
+        statuses = self._statuses(state)
         pos = self.next_position
         for i in range(length):
             logits = self._step(questions[:, i], pos, state)
@@ -144,8 +161,10 @@ class Answerer:
             want = torch.full((n,), kept, dtype=torch.int32, device=self.device)
             for p, t, scores in zip(pools, thin, state["scores"]):
                 # the question itself stays, and the first rows, which draw attention whatever they show
-                new = cache.sttm_cache_evict(p, t, state["lengths"], want, scores, kept, first=4, last=length).new_lengths
-            state = self._state(thin, new, False)
+                left = cache.sttm_cache_evict(p, t, state["lengths"], want, scores, kept, first=4, last=length)
+                statuses.append(left.status)
+            state = self._state(thin, left.new_lengths, False)
+            statuses += self._statuses(state)
         answers = []
         for _ in range(answer_tokens):
             tokens = logits.argmax(-1)
@@ -154,6 +173,7 @@ class Answerer:
                 logits = self._step(tokens, pos, state)
                 pos += 1
         self.logits = logits
+        _check_status("Answerer.ask", statuses)
         return torch.stack(answers, 1)
 
 
