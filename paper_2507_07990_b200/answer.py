@@ -59,6 +59,7 @@ class Answerer:
                             out=mat(c.q_heads * c.dim, c.width), norm2=one(c.width), up=mat(c.width, 2 * c.hidden), down=mat(c.hidden, c.width))
                        for _ in range(c.layers)]
         self.norm, self.embed, self.head = one(c.width), mat(c.vocab, c.width) * c.vocab ** 0.5, mat(c.width, c.vocab)
+        self.pools: List[cache.PagedCache] = []                  # one per layer, once a video has been watched
         half = c.dim // 2
         self.rotary = cache.Rotary((c.theta ** (-torch.arange(half, dtype=torch.float64) / half)).float().to(device))
 
@@ -86,7 +87,7 @@ class Answerer:
         self.shared = n // c.page                                # full pages
         x, positions = merged.out_feats[:n], merged.out_pos[:n]
         offsets = torch.tensor([0, n], device=self.device)
-        self.pools: List[cache.PagedCache] = []
+        self.pools = []
         statuses = [merged.device_status]
         for layer in self.layers:
             pool = cache.empty_cache(1, n, c.kv_heads, c.dim, c.page, c.dtype, self.device)
@@ -145,6 +146,10 @@ class Answerer:
     def ask(self, questions: torch.Tensor, answer_tokens: int, keep: Optional[int] = None) -> torch.Tensor:
         """``questions`` ``[questions, length]`` token ids; ``keep``: slots that every cache keeps when the questions have
         been read (None: all).  Returns greedy answers ``[questions, answer_tokens]``."""
+        if questions.dim() != 2 or 0 in questions.shape or answer_tokens < 1 or (keep is not None and keep < 1):
+            raise ValueError("questions must be [questions, length] of at least one token each, answer_tokens and keep at least 1")
+        if not self.pools:
+            raise ValueError("no video has been watched")
         n, length = questions.shape
         pools = self._question_caches(n, length + answer_tokens)
         lengths = torch.full((n,), self.rows, dtype=torch.int32, device=self.device)
