@@ -87,20 +87,21 @@ class Answerer:
         self.shared = n // c.page                                # full pages
         x, positions = merged.out_feats[:n], merged.out_pos[:n]
         offsets = torch.tensor([0, n], device=self.device)
-        self.pools = []
+        self.pools, pools = [], []
         statuses = [merged.device_status]
         for layer in self.layers:
             pool = cache.empty_cache(1, n, c.kv_heads, c.dim, c.page, c.dtype, self.device)
             q, k, v = self._qkv(layer, x)
             entered = self._append_plan(pool, layer).run(q, k, v, offsets, None, positions)
             q = entered.q
-            self.pools.append(pool)
+            pools.append(pool)
             statuses.append(entered.status)
             # the video's own attention, from the cache's keys and values in slot order
             ks, vs = (t.transpose(1, 2).reshape(-1, c.kv_heads, c.dim)[:n].transpose(0, 1).unsqueeze(0) for t in (pool.k, pool.v))
             att = F.scaled_dot_product_attention(q.transpose(0, 1).unsqueeze(0), ks, vs, is_causal=True, enable_gqa=True)
             x = self._rest(layer, x, att[0].transpose(0, 1))
         _check_status("Answerer.watch", statuses)
+        self.pools = pools
         return n
 
     def _question_caches(self, questions: int, more: int) -> List[cache.PagedCache]:

@@ -35,3 +35,14 @@ def test_a_video_that_its_cache_has_no_room_for(monkeypatch):
     with pytest.raises(binding.SttmError) as e:
         watch()
     assert e.value.code == 4
+
+
+def test_a_video_that_failed_leaves_nothing_to_ask(monkeypatch):
+    model = watch()
+    real = answer.cache.empty_cache
+    monkeypatch.setattr(answer.cache, "empty_cache", lambda seqs, n, *more: real(seqs, n - 16, *more))
+    video = helpers.to_torch(inputs.make_video(helpers.small_spec(72, 8, 13, 13, 256, p_static=0.8)))
+    with pytest.raises(binding.SttmError):
+        model.watch(video, 0.97, 0.9)
+    with pytest.raises(ValueError):
+        model.ask(questions(model), 1)
