@@ -128,11 +128,47 @@ sttm_status make_cache_map(const sttm_cache* c, void* base, int box, CUtensorMap
 }
 
 // Rows go to clusters (one launch, no parts in memory) up to so many tiles per CTA; beyond, equal shares spread them over
-// more SMs.  4 rows in clusters of 16: 4096 slots 10.5 us against 10.5 to 11.5 (the second launch's cost on the host varies), 8192
-// slots 12.9 against 11.9.  Where the rows alone occupy half of the GPU's CTAs, a CTA takes a row up to kWholeTiles tiles: 256 rows
-// of 512 slots 18 us against 30, of 1024 30 against 41; of 2048 53 both ways.  With scores only the latter: a cluster's
-// few threads take longer over the scores than the launch that spares them (4 rows of 4096 slots: 13.2 us against 12.1).
+// more SMs.  Clusters / shares in us, 128 channels, seven heads per KV head, more caches in turn than L2 holds:
+//   tiles per CTA              4             6             8            12
+//   1 row, 16 CTAs         9.8 /  9.7   11.6 / 10.4   12.8 / 11.7   16.2 / 14.1
+//   4 rows, 16 CTAs       11.3 / 12.7   12.7 / 13.9   13.9 / 14.0   16.7 / 16.1
+//   8 rows, 16 CTAs       13.0 / 14.1   14.9 / 16.3   16.4 / 17.6   20.0 / 20.2
+//   16 rows, 8 CTAs       12.6 / 14.2                 15.8 / 17.6   19.5 / 20.2
+//   32 rows, 4 CTAs       12.2 / 13.8                 15.3 / 17.2
+// The edge lies at 4 tiles for one row, at 8 for four, and beyond 12 from eight rows on; six is between.  Where the rows alone
+// occupy half of the GPU's CTAs, a CTA takes a row up to kWholeTiles tiles: 256 rows of 512 slots 18.2 us against 22.5, of 1024 29.5
+// against 33.7, of 4096 85.5 against 90.7; with scores 24.4 / 28.3, 41.9 / 42.0, and from there on shares win (1536: 57.4 / 54.9),
+// so 16 tiles.  With scores only the latter: a cluster's few threads take longer over the scores than the
+// launch that spares them.
 constexpr int kClusterTiles = 6, kWholeTiles = 16;
+
+// Clusters of `size` CTAs with an SM each (heads of 256 channels) that the GPU holds at once.  Fewer than its SMs over
+// `size`, since a cluster lies in one group of SMs whose number it need not divide: 15 of 8 CTAs, 33 of 4, 74 of 2 on 148 SMs.  (Two CTAs
+// to an SM leave room: 14 clusters of 16, 33 of 8.)
+int resident_clusters(int size) {
+    static int cached[kMaxDevices][kAttMaxCluster + 1] = {};
+    const int dev = device_slot();
+    if (dev < 0) return sm_count() / size;
+    int& n = cached[dev][size];
+    if (n == 0) {
+        const auto kernel = k_cache_attend<__nv_bfloat16, 256, 16>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)size);
+        cfg.blockDim = dim3(kAttThreads);
+        cfg.dynamicSmemBytes = attend_stages(256) * (size_t)kAttStage + attend_fixed_bytes<256, 16>();
+        cudaLaunchAttribute at;
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = (unsigned)size;
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        static size_t allowed[kMaxDevices] = {};
+        if (allow_smem((const void*)kernel, cfg.dynamicSmemBytes, allowed) != STTM_OK ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1)
+            n = sm_count() / size;
+    }
+    return n;
+}
 
 struct AttendPlan {
     int cluster;                  // see AttendArgs
@@ -157,10 +193,13 @@ sttm_status plan_attend(const sttm_cache* c, const sttm_attend_params* p, Attend
     if (pl->tiles > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
     pl->grid_limit = sm_count() * (c->dim == 256 ? 1 : 2);
     // The largest cluster that leaves every CTA a tile and, over all rows, an SM.  16 CTAs want 8 SMs of one GPC, or 16
-    // where an SM holds one CTA: there 8 have to do.
+    // where an SM holds one CTA: there 8 have to do, and fewer where the rows' clusters would not be resident at once (16 rows
+    // of 1024 slots took 23.0 us in clusters of 8, in two goes; 14.7 in shares).
     const int most = c->dim == 256 ? 8 : kAttMaxCluster;
     int size = 1;
     while (size < most && size < pl->row_tiles && rows * size * 2 <= sm_count()) size *= 2;
+    if (c->dim == 256)
+        while (size > 1 && rows > resident_clusters(size)) size /= 2;
     const bool many = rows * 2 > pl->grid_limit;
     pl->cluster = pl->row_tiles <= size * (many ? kWholeTiles : kClusterTiles) && (many || p->scores == nullptr) ? size : 0;
     // blocks per row that update scores: one go each while all of them are resident at once
@@ -314,8 +353,7 @@ sttm_status sttm_cache_attend(const sttm_cache* cache, const sttm_attend_params*
     return by_type(cache, [&](auto tag, auto dim) {
         using T = decltype(tag);
         constexpr int D = decltype(dim)::value;
-        // two CTAs to an SM with 96 KB of stages each, or one with 192 KB (256 channels)
-        a.stages = D == 256 ? 6 : 3;
+        a.stages = attend_stages(D);
         sttm_status r = a.group <= 8 ? launch_attend<T, D, 8>(a, pl, mk, mv, stream) : launch_attend<T, D, 16>(a, pl, mk, mv, stream);
         if (r != STTM_OK || pl.cluster) return r;
         return launch(k_cache_join<T, D>, pl.join_grid, kJoinThreads, 0, 0, stream, a, (int)pl.join_blocks, pl.chunks);

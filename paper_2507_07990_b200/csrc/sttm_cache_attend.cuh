@@ -38,6 +38,8 @@ namespace sttm {
 
 // Slots per tile: 32 KB of keys and values whatever the head's channels.
 __host__ __device__ constexpr int attend_tile(int dim) { return 8192 / dim; }
+// stages of a CTA's ring: two CTAs to an SM with 96 KB each, or one with 192 KB
+__host__ __device__ constexpr int attend_stages(int dim) { return dim == 256 ? 6 : 3; }
 constexpr uint32_t kAttStage = 32768;                       // bytes of a stage: a tile's keys, then its values
 constexpr int kAttWarps = 4;                                // consumer warps
 constexpr int kAttAhead = 1;                                // matrix fragments are loaded so many products ahead

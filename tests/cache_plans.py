@@ -8,7 +8,7 @@ def stages(dim):
 
 def attend_split(lens, heads, dim, max_len, scored, masked, sms=148):
     """{"cluster": CTAs per row, "each": tiles of a CTA} or {"cluster": 0, "each", "with_rows", "parts": per non-empty row, if shares
-    end with rows}."""
+    end with rows}.  (At 256 channels: as long as the rows' clusters fit the GPU at once.)"""
     up = lambda a, b: -(-a // b)
     tile = 8192 // dim
     rows, row_tiles, limit = len(lens) * heads, up(max_len, tile), sms * (1 if dim == 256 else 2)

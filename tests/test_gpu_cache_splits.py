@@ -152,6 +152,25 @@ def test_attend_large_clusters_at_their_longest(dim, size, group):
     check_rows(p, base.run_attend(p), None)
 
 
+def shares_workspace(rows, n, group, dim):
+    """The split of `rows` rows of n slots in one sequence, by its workspace: only shares keep parts of rows there."""
+    pool = cache.empty_cache(1, n, rows, dim)
+    plan = cache.AttendPlan(pool, rows * group, max_len=n)
+    ws = plan._workspace(False)[1]
+    tiles = rows * -(-n // (8192 // dim))
+    return ws >= (min(sms() * (1 if dim == 256 else 2), tiles) + rows) * group * dim * 4
+
+
+def test_attend_clusters_of_one_cta_to_an_sm_have_to_fit_at_once():
+    """A cluster lies in one group of SMs: 16 clusters of 8 CTAs that want an SM each do not fit 148 SMs."""
+    assert not shares_workspace(8, 1024, 7, 256) and not shares_workspace(4, 1024, 7, 256)
+    for rows in (16, 18, 36):
+        assert shares_workspace(rows, 1024, 7, 256)
+    for rows, n in ((16, 1024), (16, 512), (18, 700), (36, 300)):
+        p = base.attend_problem(77, [n, n - 3], q_heads=3 * rows // 2, heads=rows // 2, dim=256, page=32)
+        check_rows(p, base.run_attend(p), None)
+
+
 def test_attend_gives_the_same_bits_every_time():
     for name, group, masked in (("forty128", 7, False), ("forty128", 7, True), ("uneven256", 20, False)):
         lens, heads, dim = LONG[name]
