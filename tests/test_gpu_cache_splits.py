@@ -152,23 +152,33 @@ def test_attend_large_clusters_at_their_longest(dim, size, group):
     check_rows(p, base.run_attend(p), None)
 
 
-def shares_workspace(rows, n, group, dim):
-    """The split of `rows` rows of n slots in one sequence, by its workspace: only shares keep parts of rows there."""
-    pool = cache.empty_cache(1, n, rows, dim)
-    plan = cache.AttendPlan(pool, rows * group, max_len=n)
-    ws = plan._workspace(False)[1]
-    tiles = rows * -(-n // (8192 // dim))
-    return ws >= (min(sms() * (1 if dim == 256 else 2), tiles) + rows) * group * dim * 4
+def attend_launches(rows, n, dim):
+    plan = cache.AttendPlan(cache.empty_cache(1, n, rows, dim, 32), rows, max_len=n)
+    q, lengths = torch.zeros((1, rows, dim), dtype=torch.bfloat16, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    return plans.launches(lambda: plan.run(q, lengths))
 
 
-def test_attend_clusters_of_one_cta_to_an_sm_have_to_fit_at_once():
-    """A cluster lies in one group of SMs: 16 clusters of 8 CTAs that want an SM each do not fit 148 SMs."""
-    assert not shares_workspace(8, 1024, 7, 256) and not shares_workspace(4, 1024, 7, 256)
-    for rows in (16, 18, 36):
-        assert shares_workspace(rows, 1024, 7, 256)
-    for rows, n in ((16, 1024), (16, 512), (18, 700), (36, 300)):
-        p = base.attend_problem(77, [n, n - 3], q_heads=3 * rows // 2, heads=rows // 2, dim=256, page=32)
-        check_rows(p, base.run_attend(p), None)
+@pytest.mark.parametrize("rows,n", [(4, 1024), (8, 1024), (16, 1024), (16, 512), (18, 700), (36, 300)])
+def test_attend_clusters_have_to_fit_at_once(rows, n):
+    """A cluster lies in one group of SMs, whose number it need not divide.  Where a CTA of 256 channels takes an SM, rows whose
+    clusters are not all resident would run in two goes."""
+    made = attend_launches(rows, n, 256)
+    size = made[0].grid[0] // rows if len(made) == 1 else 0
+    assert size > 1 or rows > 8
+    assert size <= 1 or (made[0].grid[0] == rows * size and plans.resident_clusters(made[0], size) >= rows)
+    p = base.attend_problem(77, [n, n - 3], q_heads=3 * rows // 2, heads=rows // 2, dim=256, page=32)
+    check_rows(p, base.run_attend(p), None)
+
+
+@pytest.mark.parametrize("dim,rows,n,size", [(64, 1, 4096, 16), (128, 4, 6144, 16), (128, 9, 3000, 16), (128, 18, 2000, 8), (64, 37, 2000, 4),
+                                             (256, 4, 1536, 8), (256, 80, 512, 1), (128, 4, 7000, 0), (64, 160, 4000, 0)])
+def test_attend_launches_the_split_that_is_worked_out(dim, rows, n, size):
+    made = attend_launches(rows, n, dim)
+    assert plans.attend_split([n], rows, dim, n, False, False, sms())["cluster"] == size
+    if size:
+        assert len(made) == 1 and made[0].grid[0] == rows * size
+    else:
+        assert len(made) == 2 and made[0].grid[0] == min(sms() * (1 if dim == 256 else 2), rows * -(-n // (8192 // dim)))
 
 
 def test_attend_gives_the_same_bits_every_time():
@@ -231,7 +241,7 @@ def test_the_sorted_definition_is_the_plain_one():
 @pytest.mark.parametrize("kind", ["weights", "ties", "odd"])
 @pytest.mark.parametrize("seqs,heads,n,split", [
     (25, 3, 3000, (1, 3)), (25, 3, 9000, (1, 9)), (16, 8, 16421, (1, 17)), (25, 3, 25000, (1, 25)), (25, 3, 33000, (1, 33)),
-    (2, 1, 6144, (2, 3)), (2, 1, 3073, (2, 3)), (20, 2, 9000, (2, 9)), (20, 2, 25000, (2, 17)), (18, 2, 50001, (4, 17)), (20, 2, 70000, (4, 25)),
+    (2, 1, 6144, (2, 3)), (2, 1, 3073, (2, 3)), (20, 2, 9000, (2, 9)), (20, 2, 25000, (2, 17)), (14, 2, 50001, (4, 17)), (20, 2, 70000, (4, 25)),
     (1, 2, 25001, (8, 9)), (2, 1, 130000, (8, 17)), (1, 2, 199999, (8, 25)), (1, 2, 270000, (8, 33)),
 ], ids=str)
 def test_evict_every_split(seqs, heads, n, split, kind):
@@ -240,6 +250,29 @@ def test_evict_every_split(seqs, heads, n, split, kind):
     p = base.evict_problem(81, lens, keep, heads=heads, page=64, dst_page=32, kind=kind)
     assert plans.select_split(seqs * heads, n, sms()) == split
     check_selection(p, 4, 64)
+
+
+def select_launch(rows, n):
+    src, dst = cache.empty_cache(1, n, rows, 64, 64), cache.empty_cache(1, 40, rows, 64, 64)
+    plan = cache.EvictPlan(src, dst, 40, max_len=n)
+    ints = lambda x: torch.tensor([x], dtype=torch.int32, device="cuda")
+    lengths, keep, scores = ints(n), ints(40), torch.rand((1, rows, n), device="cuda")
+    select, move = plans.launches(lambda: plan.run(lengths, keep, scores))
+    return select
+
+
+@pytest.mark.parametrize("rows,n", [(1, 6144), (15, 30000), (32, 30000), (40, 25000), (75, 9000), (2, 270000)])
+def test_evict_launches_the_split_that_is_worked_out(rows, n):
+    assert select_launch(rows, n).grid[0] == rows * plans.select_split(rows, n, sms())[0]
+
+
+@pytest.mark.parametrize("rows,n", [(16, 25000), (18, 55788), (17, 130000), (34, 25000), (37, 55788), (16, 16421)])
+def test_evict_clusters_have_to_fit_at_once(rows, n):
+    """A cluster lies in one group of SMs, whose number it need not divide: rows whose clusters are not all resident would be
+    selected from in two goes."""
+    select = select_launch(rows, n)
+    size = select.grid[0] // rows
+    assert size >= 2 and select.grid[0] == rows * size and plans.resident_clusters(select, size) >= rows
 
 
 @pytest.mark.parametrize("kind", ["weights", "ties", "odd"])
