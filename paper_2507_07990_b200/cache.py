@@ -114,7 +114,8 @@ def empty_cache(seqs: int, max_len: int, heads: int, dim: int, page: int = 64, d
 @dataclass
 class Rotary:
     """Rotation by position: ``inv_freq`` float32 ``[rot / 2]`` on the device.  Pairs are channels (i, i + rot / 2), or
-    (2 i, 2 i + 1) when ``interleaved``.  ``sections``: pairs turned by each of three positions (time, row, column)."""
+    (2 i, 2 i + 1) when ``interleaved``.  ``sections``: pairs turned by each of three positions (time, row, column), which
+    the caller makes of a merge's survived ids: ``id // (H * W)``, ``id % (H * W) // W`` and ``id % W``."""
     inv_freq: torch.Tensor
     interleaved: bool = False
     sections: Optional[Sequence[int]] = None

@@ -9,9 +9,10 @@
 // memory.
 //
 // A warp takes a row (few rows: a part of one) in steps of 1 KB and has two steps on their way into
-// shared memory while it works on one (asynchronous copies; a lane reads back what it copied itself): 158 us, 6.5 TB/s, on
-// 55724 rows of 36 heads of 128 channels.  Loads into registers, one step ahead, took 191 us (the registers cost warps); seven
-// steps on their way, 189 us (so does the shared memory, and L1 with it).
+// shared memory while it works on one (asynchronous copies; a lane reads back what it copied itself): 159 us, 6.5 TB/s, on
+// 55724 rows of 36 heads of 128 channels in the first calls at 1965 MHz; call after call the power limit has the clock at 1.7 GHz,
+// where the instructions bound it: 175 to 183 us, 5.7 TB/s.  In first calls loads into registers, one step ahead, took 191 us (the
+// registers cost warps); seven steps on their way, 189 us (so does the shared memory, and L1 with it).
 #pragma once
 
 #include "sttm_cache.cuh"

@@ -11,13 +11,14 @@
 // sequence or many ragged ones keep every SM streaming equally long; a row that lies in several shares leaves a running
 // maximum, a sum and an unscaled output per share, joined in share order by k_cache_join (no atomics: the bits of a
 // result do not depend on scheduling).  Clusters: a row is cut evenly over the 1 to 16 CTAs of a cluster, which join
-// their parts in shared memory, one launch in all.  5338 slots of 4 KV heads: 11.9 us in clusters of 16, 14 us in shares.
+// their parts in shared memory, one launch in all.  5338 slots of 4 KV heads, out of HBM: 12.5 us in clusters of 16, 13.4 us in
+// shares.
 //
 // *Pipeline.*  A producer warp brings a tile's keys and values (32 KB) into a ring of shared-memory stages by tensor
 // copies, one box of slots that lie in one page per copy, under the 128-byte swizzle; boxes whose slots are all masked
 // are not copied.  Four warps take 32 slots at a time and never wait for one another before the end of a row: each keeps
-// its own maximum, sum and output.  32 x 32700 slots of 8 KV heads (4.3 GB) stream at 6.9 TB/s, as fast as this memory
-// reads; with scores (their logits are written and read once more, 0.5 GB) the call takes 732 us instead of 620.
+// its own maximum, sum and output.  32 x 32700 slots of 8 KV heads (4.3 GB) stream in 609 us, 7.0 TB/s, as fast as this memory
+// reads; with scores (their logits are written and read once more, 0.5 GB) the call takes 747 to 789 us.
 //
 // *Products.*  S = Q K^T and O += P V on mma.sync m16n8k16 with fp32 sums.  P is not rounded to 16 bits: it enters as
 // hi + lo, two 16-bit numbers that hold 16 bits of it (22 in fp16).  With at most 8 heads (ROWS = 8) the remainder travels
@@ -25,7 +26,13 @@
 // weights down to 2^-29 of the largest stay clear of the subnormals.  A warp needs some 1800 cycles for its 32 slots of
 // 128 channels, a quarter of the time that HBM needs for an SM's share of them: the fifth-generation products, whose
 // accumulators would have to travel through tensor memory twice per tile, have nothing to win here (the tensor pipe is busy
-// 19 % of the streaming time).
+// 19 % of the streaming time).  That holds up to 16 query heads per KV head.  Beyond, two or four sets of warps load every tile's
+// fragments each for itself, and the products bound the kernel: 8 x 32768 slots of 4 KV heads of 128 channels take 92 us with up to 16 heads
+// (5.8 TB/s), 127 with 32 (4.2), 219 with 64 (2.4); 64 channels 90, 131 and 228; 256 channels (8 x 8192 slots, 0.27 GB) 54 with 8, 59 with 16,
+// 90 with 32, 159 with 64.
+//
+// *Registers.*  Two CTAs of five warps leave 168 a thread at 128 channels, of which 172 to 220 bytes spill; one CTA at 256 channels has 255 and
+// spills 280 to 312 (64 channels: none).
 #pragma once
 
 #include <cuda.h>
