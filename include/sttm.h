@@ -61,7 +61,7 @@ typedef enum {
     STTM_ERR_TIMEOUT = 7         /* a bounded wait inside a kernel ran out (device)     */
 } sttm_status;
 
-typedef enum { STTM_BF16 = 0, STTM_F32 = 1, STTM_F16 = 2 /* cache calls only */ } sttm_dtype;
+typedef enum { STTM_BF16 = 0, STTM_F32 = 1, STTM_F16 = 2 /* cache and layer calls only */ } sttm_dtype;
 /* Section 3.4: keep the surviving token's original position, or renumber 0..N_ST-1. */
 typedef enum { STTM_POS_SURVIVED = 0, STTM_POS_REASSIGNED = 1 } sttm_pos_mode;
 /* Averaging weights inside a chain (the paper does not fix them): one per node, or the
@@ -415,6 +415,111 @@ typedef struct sttm_evict_params {
     int32_t* device_status;       /* may be NULL; also 1 << STTM_ERR_ARG (a page that is not there: not copied) */
 } sttm_evict_params;
 sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const sttm_evict_params* p, void* stream);
+
+/*
+ * Attention of new tokens of several sequences (questions) over a prefix that they share (a merged video), which is read once for
+ * all of them, and over the sequences' own slots.  `prefix` has a table row per prefix, `own` (or NULL) one per
+ * sequence; both have the same heads, dim and dtype, and may lie in the same pools.  Sequence b's new tokens are the rows
+ * row_offsets[b] ... row_offsets[b + 1] - 1, sequences seq_offsets[p] ... seq_offsets[p + 1] - 1 share prefix p (a sequence of
+ * none has its own slots only).  Token i of sequence b's n new tokens sees all slots below prefix_lengths[p] and own slots
+ * s < lengths[b] - n + i + 1 (its own key and value were appended before).
+ *   out[row, h] = sum over them of softmax(scale q[row, h] . k[s, h / group]) v[s, h / group]
+ * A row that sees no slot gives out = 0 and lse = -inf; rows of no sequence are left as they are.  What lies in slots behind a
+ * length does not matter.  A value that is not finite in a slot below a length reaches every new token of its sequences.
+ */
+typedef struct sttm_prefix_params {
+    const void* q;                /* [rows][q_heads][dim], 16-byte aligned                         */
+    long long q_row, q_head;      /* strides in elements, multiples of 8                           */
+    long long rows;               /* rows behind q, below 2^31                                     */
+    int q_heads;                  /* a multiple of the cache's heads, at most 64 per KV head       */
+    int seqs;
+    const int64_t* row_offsets;   /* [seqs + 1], not decreasing                                    */
+    const int32_t* seq_offsets;   /* [prefix->seqs + 1], not decreasing; NULL: all share prefix 0, the only one */
+    const int32_t* prefix_lengths;     /* [prefix->seqs] slots in use                              */
+    const int32_t* lengths;       /* [seqs] own slots in use, the new tokens' among them (with own) */
+    int max_prefix, max_own;      /* no length is larger (else it is cut and 1 << STTM_ERR_CAPACITY raised); at most what the
+                                     tables have room for, and below 2^31 - 2^20                   */
+    float scale;                  /* above 0                                                       */
+    void* out;                    /* [rows][q_heads][dim] contiguous, 16-byte aligned              */
+    float* lse;                   /* [rows][q_heads] log of the sum of exp(scale q . k), may be NULL */
+    int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_CAPACITY (also: offsets beyond the rows), 1 << STTM_ERR_ARG
+                                     (a page that is not there: read as zeros; offsets that decrease: nothing is written),
+                                     1 << STTM_ERR_TIMEOUT */
+} sttm_prefix_params;
+/* Workspace of a call: depends on rows, seqs, q_heads and the caches; any contents; 256-byte aligned.  0 on bad params. */
+size_t sttm_prefix_workspace_bytes(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p);
+sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/*
+ * ---- The rest of a decoder layer ----
+ *
+ * Between two blocks: for every row
+ *   r = residual_scale * residual + gate * N(x; post_norm)      sum = r      out = N(r; pre_norm)
+ * with N(y; w) = y / sqrt(mean y^2 + eps) * w, or y itself where w is NULL.  All but x may be left out: no residual is 0, no
+ * gate 1; gate and gate_rows both count where both are given.  `out` is normed from r before it is rounded to `sum`.  q and
+ * q_scale hold `out` in 8 bits (see sttm_quantize_rows).  Outputs may take the place of inputs row by row (same address and
+ * row stride); otherwise the memory from an output's first row to its last and that of any other array do not overlap.  Squares are
+ * summed in 32 bits.
+ */
+typedef struct sttm_norm_params {
+    const void* x;                /* [rows][dim] the block's output                                */
+    const void* residual;         /* [rows][dim] or NULL                                           */
+    const void* gate_rows;        /* [rows][dim] or NULL                                           */
+    long long x_row, residual_row, gate_row;     /* strides in elements, at least dim              */
+    long long rows;
+    int dim;                      /* at most 16384                                                 */
+    int dtype;                    /* of x, residual, gate_rows, sum and out: STTM_BF16, STTM_F32 or STTM_F16 */
+    const float *post_norm, *gate, *pre_norm;    /* [dim] or NULL                                  */
+    float residual_scale, eps;
+    void* sum;                    /* [rows][dim] out, or NULL                                      */
+    void* out;                    /* [rows][dim] out, or NULL                                      */
+    long long sum_row, out_row;   /* strides in elements                                           */
+    int8_t* q;                    /* [rows][dim] out, or NULL                                      */
+    long long q_row;              /* bytes                                                         */
+    float* q_scale;               /* [rows] out (with q)                                           */
+} sttm_norm_params;
+sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream);
+
+/*
+ * Rows in 8 bits with a scale each: q[t][i] = rint(y[t][i] * 127 / m), scale[t] = m / 127, m = max over i of |y[t][i]|, with
+ * y = x, or y = silu(a) * b for rows x = [a | b] (gated, x is [rows][2 dim]).  A row with an infinity or a NaN gives zeros
+ * and the scale NaN; a row whose m is below 2^-100 zeros and the scale 0.
+ */
+typedef struct sttm_quantize_params {
+    const void* x;
+    long long x_row;              /* stride in elements, at least dim (gated: 2 dim)               */
+    long long rows;
+    int dim;                      /* at most 16384                                                 */
+    int dtype;                    /* of x                                                          */
+    int gated;
+    int8_t* q;                    /* [rows][dim] out                                               */
+    long long q_row;              /* bytes                                                         */
+    float* scale;                 /* [rows] out                                                    */
+} sttm_quantize_params;
+sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream);
+
+/*
+ * Matrix product of 8-bit rows: out[t][n] = x_scale[t] * w_scale[n] * (sum over k of x[t][k] * w[n][k]) + bias[n], the sums
+ * exact, one rounding to out's type.  Both operands are [rows][inner] with 16-byte aligned rows; what lies between inner
+ * and the row's end does not matter.  Weights are quantized once, by sttm_quantize_rows over their output channels.
+ */
+typedef struct sttm_matmul_params {
+    const int8_t* x;              /* [rows][inner] tokens, 16-byte aligned                         */
+    long long x_row;              /* bytes, a multiple of 16                                       */
+    const float* x_scale;         /* [rows]                                                        */
+    long long rows;               /* below 2^31                                                    */
+    const int8_t* w;              /* [outer][inner] weights, 16-byte aligned                       */
+    long long w_row;              /* bytes, a multiple of 16                                       */
+    const float* w_scale;         /* [outer]                                                       */
+    int inner, outer;             /* inner at most 131056, so that no sum passes 32 bits           */
+    const float* bias;            /* [outer] or NULL                                               */
+    void* out;                    /* [rows][outer]                                                 */
+    long long out_row;            /* elements                                                      */
+    int out_dtype;                /* STTM_BF16, STTM_F32 or STTM_F16                               */
+    int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_TIMEOUT                 */
+} sttm_matmul_params;
+sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream);
 
 /* Frees the cached buffers of sttm_merge / sttm_merge_host on the current device. */
 void sttm_release_cache(void);

@@ -32,7 +32,8 @@ EXPORTS = ["sttm_default_params", "sttm_workspace_bytes", "sttm_sims_per_frame",
            "sttm_merged_positions_workspace", "sttm_merge_budget", "sttm_budget_workspace_bytes",
            "sttm_row_weights", "sttm_segment_fold", "sttm_segment_emit", "sttm_segment_finish",
            "sttm_status_from_bits", "sttm_merge_status",
-           "sttm_cache_append", "sttm_attend_workspace_bytes", "sttm_cache_attend", "sttm_cache_evict"]
+           "sttm_cache_append", "sttm_attend_workspace_bytes", "sttm_cache_attend", "sttm_cache_evict",
+           "sttm_prefix_workspace_bytes", "sttm_prefix_attend", "sttm_block_norm", "sttm_quantize_rows", "sttm_quant_matmul"]
 
 
 class SttmParams(C.Structure):
@@ -133,6 +134,13 @@ def load_library(path: Optional[str] = None):
     lib.sttm_cache_attend.restype = C.c_int
     lib.sttm_cache_evict.argtypes = [vp, vp, vp, vp]
     lib.sttm_cache_evict.restype = C.c_int
+    lib.sttm_prefix_workspace_bytes.argtypes = [vp, vp, vp]
+    lib.sttm_prefix_workspace_bytes.restype = C.c_size_t
+    lib.sttm_prefix_attend.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
+    lib.sttm_prefix_attend.restype = C.c_int
+    for name in ("sttm_block_norm", "sttm_quantize_rows", "sttm_quant_matmul"):
+        getattr(lib, name).argtypes = [vp, vp]
+        getattr(lib, name).restype = C.c_int
     lib.sttm_status_string.argtypes = [C.c_int]
     lib.sttm_status_string.restype = C.c_char_p
     if path == _build.LIB_PATH:

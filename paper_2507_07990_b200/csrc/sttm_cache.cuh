@@ -59,4 +59,19 @@ struct Pair<__half> {
     }
 };
 
+// sequence of a row: the number of offsets [1 .. seqs] that are <= row, found by the whole warp, 32 probes a step
+template <typename I>
+__device__ __forceinline__ int sequence_of(const I* offsets, int seqs, long long row, int lane) {
+    int lo = 0, n = seqs;                                   // answer in [lo, lo + n]
+    while (n > 0) {
+        const int step = (n + 31) / 32;                     // probe offsets lo + step, lo + 2 step, ...
+        const int at = lo + (lane + 1) * step;
+        const bool below = at <= lo + n && offsets[at] <= row;
+        const int hits = __popc(__ballot_sync(0xffffffffu, below));
+        lo += hits * step;
+        n = min(step - 1, n - hits * step);
+    }
+    return min(lo, seqs - 1);
+}
+
 }  // namespace sttm

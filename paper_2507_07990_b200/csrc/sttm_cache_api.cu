@@ -15,10 +15,6 @@ namespace {
 
 using namespace sttm;
 
-// Slots of a row at most: the kernels count them in 32 bits and step up to sm_count() * 4096 beyond the last
-// (148 multiprocessors: 606208).
-constexpr int kMaxSlots = INT_MAX - (1 << 20);
-
 // Do rows of `len` numbers, `seq` elements from one sequence to the next and `head` from one of its heads to the next, share any?
 // (One axis has to lie inside the other's stride; the stride of an axis of length one says nothing.)
 bool rows_overlap(long long seq, long long head, int seqs, int heads, int len) {

@@ -44,20 +44,6 @@ struct AppendArgs {
 constexpr int kAppendWarps = 4;
 constexpr int kAppendRing = 3;          // steps: two on their way, one being read
 
-// sequence of a row: the number of offsets [1 .. seqs] that are <= row, found by the whole warp, 32 probes a step
-__device__ __forceinline__ int sequence_of(const long long* offsets, int seqs, long long row, int lane) {
-    int lo = 0, n = seqs;                                   // answer in [lo, lo + n]
-    while (n > 0) {
-        const int step = (n + 31) / 32;                     // probe offsets lo + step, lo + 2 step, ...
-        const int at = lo + (lane + 1) * step;
-        const bool below = at <= lo + n && offsets[at] <= row;
-        const int hits = __popc(__ballot_sync(0xffffffffu, below));
-        lo += hits * step;
-        n = min(step - 1, n - hits * step);
-    }
-    return min(lo, seqs - 1);
-}
-
 __device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }

@@ -42,6 +42,10 @@ inline sttm_status allow_smem(const void* kernel, size_t bytes, size_t (&allowed
     return STTM_OK;
 }
 
+// Slots of a row at most: the kernels count them in 32 bits and step up to sm_count() * 4096 beyond the last
+// (148 multiprocessors: 606208).
+constexpr int kMaxSlots = INT_MAX - (1 << 20);
+
 inline bool multiple_of_8(long long v) { return v % 8 == 0; }
 // is any of these arrays of 4-byte numbers (or NULL) at an address that is no multiple of 4?
 template <typename... P>

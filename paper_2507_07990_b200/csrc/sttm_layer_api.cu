@@ -1,0 +1,209 @@
+// Host side of a decoder layer's calls (sttm_block_norm, sttm_quantize_rows, sttm_quant_matmul): argument checks, choice of the
+// kernel's form, launches.
+#include "../../include/sttm.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "sttm_block_norm.cuh"
+#include "sttm_cache_host.cuh"
+#include "sttm_quant_matmul.cuh"
+
+namespace {
+
+using namespace sttm;
+
+bool known_type(int dtype) { return dtype == STTM_BF16 || dtype == STTM_F16 || dtype == STTM_F32; }
+
+// a call of `f` with the element type as a value
+template <typename F>
+sttm_status by_element(int dtype, F&& f) {
+    return dtype == STTM_BF16 ? f(__nv_bfloat16()) : dtype == STTM_F16 ? f(__half()) : f(0.0f);
+}
+
+// Threads per row and chunks per thread: the fewest threads that hold a row in so many chunks each (four of 16 bytes, 16 single
+// elements where rows do not fill whole 16-byte words).
+template <typename T, int VEC, bool QUANTIZE>
+sttm_status launch_rows(const NormArgs& a, void* stream) {
+    constexpr int NCH = VEC == 1 ? 16 : VEC == 4 ? 8 : 4;
+    auto go = [&](auto tpr) -> sttm_status {
+        constexpr int TPR = decltype(tpr)::value, BLOCK = kNormBlock<T, VEC, TPR>, PER = BLOCK / TPR;
+        const long long grid = (a.rows + PER - 1) / PER;
+        if constexpr (QUANTIZE) return launch(k_quantize_rows<T, VEC, TPR, NCH>, grid, BLOCK, 0, 0, stream, a);
+        else return launch(k_block_norm<T, VEC, TPR, NCH>, grid, BLOCK, 0, 0, stream, a);
+    };
+    const int per_thread = NCH * VEC;
+    if (a.dim <= 32 * per_thread) return go(std::integral_constant<int, 32>());
+    if (a.dim <= 128 * per_thread) return go(std::integral_constant<int, 128>());
+    if (a.dim <= 256 * per_thread) return go(std::integral_constant<int, 256>());
+    if (a.dim <= 512 * per_thread) return go(std::integral_constant<int, 512>());
+    return go(std::integral_constant<int, 1024>());
+}
+
+struct MatmulPlan {
+    bool swap;                    // weights are the 128-row operand
+    int nt, cluster, stages;
+    long long a_tiles, b_tiles, grid;
+};
+
+MatmulPlan plan_matmul(const sttm_matmul_params* p) {
+    MatmulPlan pl;
+    const int blocks = (p->inner + kMatK - 1) / kMatK, sms = sm_count();
+    pl.swap = p->rows <= 256;
+    pl.nt = 256;
+    if (pl.swap)
+        for (pl.nt = 16; pl.nt < p->rows;) pl.nt *= 2;
+    const long long a_rows = pl.swap ? p->outer : p->rows, b_rows = pl.swap ? p->rows : p->outer;
+    pl.a_tiles = (a_rows + 127) / 128;
+    pl.b_tiles = (b_rows + pl.nt - 1) / pl.nt;
+    const long long tiles = pl.a_tiles * pl.b_tiles;
+    // two CTAs to an SM where their rings and accumulators fit
+    const int per_sm = pl.nt <= 64 ? 2 : 1;
+    pl.stages = std::min(kMatMaxStages, (int)((227 * 1024 / per_sm - 1024 - matmul_fixed_bytes()) / matmul_slot(pl.nt)));
+    pl.cluster = 1;
+    if (pl.swap)
+        while (pl.cluster < 8 && tiles * pl.cluster * 2 <= (long long)sms * per_sm && blocks >= 4 * pl.cluster) pl.cluster *= 2;
+    pl.grid = pl.cluster > 1 ? tiles * pl.cluster : std::min<long long>(tiles, (long long)sms * per_sm);
+    return pl;
+}
+
+sttm_status make_rows_map(const void* base, long long rows, int inner, long long row_bytes, int box_rows, CUtensorMap* map) {
+    const EncodeTiledFn encode = tensor_map_encoder();
+    if (encode == nullptr) return STTM_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {kMatK, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? STTM_OK : STTM_ERR_UNSUPPORTED;
+}
+
+template <typename T, int NT, bool SWAP>
+sttm_status launch_matmul(const MatmulArgs& a, const MatmulPlan& pl, const CUtensorMap& ma, const CUtensorMap& mb, void* stream) {
+    static size_t allowed[kMaxDevices] = {};
+    const size_t smem = (size_t)pl.stages * matmul_slot(NT) + matmul_fixed_bytes();
+    const sttm_status s = allow_smem((const void*)k_quant_matmul<T, NT, SWAP>, smem, allowed);
+    return s != STTM_OK ? s : launch(k_quant_matmul<T, NT, SWAP>, pl.grid, kMatThreads, smem, pl.cluster > 1 ? pl.cluster : 0, stream, a, ma, mb);
+}
+
+// Do two arrays of `rows` rows share memory, other than one in the other's place?
+bool clash(const void* out, long long out_row, const void* in, long long in_row, long long rows, long long width) {
+    if (out == nullptr || in == nullptr || (out == in && (out_row == in_row || rows == 1))) return false;
+    const uintptr_t o = (uintptr_t)out, i = (uintptr_t)in;
+    return o < i + (uintptr_t)((rows - 1) * in_row + width) && i < o + (uintptr_t)((rows - 1) * out_row + width);
+}
+
+}  // namespace
+
+extern "C" {
+
+sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream) {
+    if (p == nullptr || p->rows < 0 || p->dim < 1 || !known_type(p->dtype)) return STTM_ERR_ARG;
+    if (p->dim > kNormMaxDim || p->rows > INT_MAX) return STTM_ERR_UNSUPPORTED;
+    if (p->sum == nullptr && p->out == nullptr && p->q == nullptr) return STTM_ERR_ARG;
+    if ((p->q == nullptr) != (p->q_scale == nullptr) || !std::isfinite(p->residual_scale) || !(p->eps >= 0.0f)) return STTM_ERR_ARG;
+    if (p->rows == 0) return STTM_OK;
+    if (p->x == nullptr) return STTM_ERR_ARG;
+    const long long e = p->dtype == STTM_F32 ? 4 : 2, width = p->dim * e;
+    const void* const in[3] = {p->x, p->residual, p->gate_rows};
+    const long long in_row[3] = {p->x_row, p->residual_row, p->gate_row};
+    const void* const out[3] = {p->sum, p->out, p->q};
+    const long long out_row[3] = {p->sum_row, p->out_row, p->q_row};
+    bool wide = p->dim % (16 / e) == 0;
+    for (int i = 0; i < 3; i++) {
+        if (in[i] != nullptr && ((p->rows > 1 && (in_row[i] < p->dim || in_row[i] > LLONG_MAX / 4 / p->rows)) || misaligned(in[i], e))) return STTM_ERR_ARG;
+        if (out[i] != nullptr && ((p->rows > 1 && (out_row[i] < p->dim || out_row[i] > LLONG_MAX / 4 / p->rows)) || (i < 2 && misaligned(out[i], e)))) return STTM_ERR_ARG;
+        wide = wide && (in[i] == nullptr || (!misaligned(in[i], 16) && (p->rows == 1 || in_row[i] * e % 16 == 0)));
+        wide = wide && (out[i] == nullptr || i == 2 || (!misaligned(out[i], 16) && (p->rows == 1 || out_row[i] * e % 16 == 0)));
+    }
+    if (odd_address(p->post_norm, p->gate, p->pre_norm, p->q_scale)) return STTM_ERR_ARG;
+    const uintptr_t weights = (uintptr_t)p->post_norm | (uintptr_t)p->gate | (uintptr_t)p->pre_norm;
+    wide = wide && weights % 16 == 0 && (p->q == nullptr || (!misaligned(p->q, 8) && (p->rows == 1 || p->q_row % 8 == 0)));
+    for (int o = 0; o < 3; o++) {
+        const long long ob = o < 2 ? out_row[o] * e : out_row[o], ow = o < 2 ? width : p->dim;
+        for (int i = 0; i < 3; i++)
+            if (o < 2 ? clash(out[o], ob, in[i], in_row[i] * e, p->rows, width)
+                      : out[o] && in[i] && (out[o] == in[i] || clash(out[o], ob, in[i], in_row[i] * e, p->rows, width))) return STTM_ERR_ARG;
+        for (int u = 0; u < o; u++)
+            if (out[o] && out[u] && (out[o] == out[u] || clash(out[o], ob, out[u], out_row[u] * e, p->rows, std::max(ow, width)))) return STTM_ERR_ARG;
+    }
+    NormArgs a = {};
+    a.x = p->x; a.residual = p->residual; a.gate_rows = p->gate_rows;
+    a.x_row = p->x_row; a.residual_row = p->residual_row; a.gate_row = p->gate_row;
+    a.post_norm = p->post_norm; a.gate = p->gate; a.pre_norm = p->pre_norm;
+    a.residual_scale = p->residual_scale;
+    a.eps = p->eps;
+    a.sum = p->sum; a.out = p->out;
+    a.sum_row = p->sum_row; a.out_row = p->out_row;
+    a.q = p->q; a.q_row = p->q_row; a.q_scale = p->q_scale;
+    a.rows = p->rows;
+    a.dim = p->dim;
+    return by_element(p->dtype, [&](auto tag) {
+        using T = decltype(tag);
+        return wide ? launch_rows<T, 16 / sizeof(T), false>(a, stream) : launch_rows<T, 1, false>(a, stream);
+    });
+}
+
+sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream) {
+    if (p == nullptr || p->rows < 0 || p->dim < 1 || !known_type(p->dtype)) return STTM_ERR_ARG;
+    if (p->dim > kNormMaxDim || p->rows > INT_MAX) return STTM_ERR_UNSUPPORTED;
+    if (p->rows == 0) return STTM_OK;
+    if (p->x == nullptr || p->q == nullptr || p->scale == nullptr || odd_address(p->scale)) return STTM_ERR_ARG;
+    const long long e = p->dtype == STTM_F32 ? 4 : 2, in = p->gated ? 2ll * p->dim : p->dim;
+    if (misaligned(p->x, e) || (p->rows > 1 && (p->x_row < in || p->q_row < p->dim || p->x_row > LLONG_MAX / 4 / p->rows || p->q_row > LLONG_MAX / 4 / p->rows)))
+        return STTM_ERR_ARG;
+    if ((const void*)p->q == p->x || clash(p->q, p->q_row, p->x, p->x_row * e, p->rows, in * e)) return STTM_ERR_ARG;
+    const bool wide = p->dim % (16 / e) == 0 && !misaligned(p->x, 16) && !misaligned(p->q, 8) && (p->rows == 1 || (p->x_row * e % 16 == 0 && p->q_row % 8 == 0));
+    NormArgs a = {};
+    a.x = p->x; a.x_row = p->x_row;
+    a.q = p->q; a.q_row = p->q_row; a.q_scale = p->scale;
+    a.rows = p->rows;
+    a.dim = p->dim;
+    a.gated = p->gated != 0;
+    return by_element(p->dtype, [&](auto tag) {
+        using T = decltype(tag);
+        return wide ? launch_rows<T, 16 / sizeof(T), true>(a, stream) : launch_rows<T, 1, true>(a, stream);
+    });
+}
+
+sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream) {
+    if (p == nullptr || p->rows < 0 || p->inner < 1 || p->outer < 1 || !known_type(p->out_dtype)) return STTM_ERR_ARG;
+    if (p->inner > 131056 || p->rows > INT_MAX) return STTM_ERR_UNSUPPORTED;
+    if (p->w == nullptr || p->w_scale == nullptr || misaligned(p->w, 16) || p->w_row % 16 != 0 || p->w_row < p->inner) return STTM_ERR_ARG;
+    if (odd_address(p->x_scale, p->w_scale, p->bias, p->device_status)) return STTM_ERR_ARG;
+    if (p->rows == 0) return STTM_OK;
+    if (p->x == nullptr || p->x_scale == nullptr || p->out == nullptr || misaligned(p->x, 16) || p->x_row % 16 != 0 || p->x_row < p->inner) return STTM_ERR_ARG;
+    const int e = p->out_dtype == STTM_F32 ? 4 : 2;
+    if (misaligned(p->out, e) || (p->rows > 1 && (p->out_row < p->outer || p->out_row > LLONG_MAX / 4 / p->rows))) return STTM_ERR_ARG;
+    const MatmulPlan pl = plan_matmul(p);
+    if (pl.a_tiles * pl.b_tiles > INT_MAX / 8) return STTM_ERR_UNSUPPORTED;
+    MatmulArgs a = {};
+    a.x_scale = p->x_scale; a.w_scale = p->w_scale; a.bias = p->bias;
+    a.out = p->out;
+    a.out_row = p->out_row;
+    a.rows = p->rows;
+    a.outer = p->outer;
+    a.blocks = (p->inner + kMatK - 1) / kMatK;
+    a.a_tiles = (int)pl.a_tiles; a.b_tiles = (int)pl.b_tiles;
+    a.cluster = pl.cluster;
+    a.stages = pl.stages;
+    a.status = p->device_status;
+    a.wide = !misaligned(p->out, 16) && (p->rows == 1 || p->out_row * e % 16 == 0);
+    CUtensorMap mx, mw;
+    sttm_status s;
+    if ((s = make_rows_map(p->x, p->rows, p->inner, p->x_row, pl.swap ? pl.nt : 128, &mx)) != STTM_OK) return s;
+    if ((s = make_rows_map(p->w, p->outer, p->inner, p->w_row, pl.swap ? 128 : pl.nt, &mw)) != STTM_OK) return s;
+    return by_element(p->out_dtype, [&](auto tag) -> sttm_status {
+        using T = decltype(tag);
+        if (!pl.swap) return launch_matmul<T, 256, false>(a, pl, mx, mw, stream);
+        switch (pl.nt) {
+            case 16: return launch_matmul<T, 16, true>(a, pl, mw, mx, stream);
+            case 32: return launch_matmul<T, 32, true>(a, pl, mw, mx, stream);
+            case 64: return launch_matmul<T, 64, true>(a, pl, mw, mx, stream);
+            case 128: return launch_matmul<T, 128, true>(a, pl, mw, mx, stream);
+            default: return launch_matmul<T, 256, true>(a, pl, mw, mx, stream);
+        }
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,685 @@
+// Attention of new tokens of several sequences over a prefix that they share and over their own slots (sttm_prefix_attend).
+//
+// With G query heads per KV head, the new tokens of all sequences of a prefix are rows (token, query head of the group) of one
+// matrix per KV head, and the prefix is read once for all of them:
+//     S = Q K^T,  P = exp2(c S - c m),  O = P V,  l = row sums of P,          c = scale * log2(e)
+// on the tensor cores (tcgen05): 128 rows and a tile of kv slots at a time, S and O in tensor memory.  A thread owns a row: it
+// takes the row's logits out of tensor memory, forms the weights and puts them back as 16-bit operand of the second product.  The
+// reference m of the exponentials follows the row's maximum only when that has risen by more than 2^8, so O is
+// rarely rescaled; weights of up to 2^8 lose nothing in 32-bit sums.  Weights enter the product in the cache's type, rounded once (half a
+// step of it, as the output is); their sum l is taken before that rounding, in 32 bits.
+//
+// Two row blocks of 128 are in work at a time (of one block, alternate tiles), so that the products of one run beside the
+// exponentials of the other: four warps per block, one that copies (queries, then key and value tiles through a ring) and one
+// that issues the products.  256-channel heads fill tensor memory with one O: there one block's tiles alternate between two
+// places for S.
+//
+// Work is cut into equal shares of tiles over all CTAs whatever the lengths are (which the host does not know): entries are the prefixes
+// and then the sequences' own slots; an entry has an item per KV head and block of rows, an item as many steps as tiles of
+// slots.  What a CTA has of an item is a piece: O, l and m of its rows go to memory, and k_prefix_join puts a row's pieces together.
+#pragma once
+
+#include "sttm_cache.cuh"
+
+namespace sttm {
+
+struct PrefixArgs {
+    CacheView prefix, own;        // own.seqs = 0: no own slots
+    int page_box[2];              // slots per tensor copy (prefix, own)
+    long long rows;
+    int q_heads, group;
+    int block_tokens;             // tokens in 128 rows: 128 / group
+    int seqs;
+    const long long* row_offsets;
+    const int32_t* seq_offsets;   // or null: one prefix
+    const int32_t *prefix_lengths, *lengths;
+    int max_prefix, max_own;
+    float scale_log2;
+    uint16_t* out;
+    float* lse;
+    int32_t* status;
+    struct PrefixHead* head;      // workspace
+    struct PrefixEntry* entries;
+    float2* stats;                // per stored row: m (times c, in powers of two) and l
+    float* partial;               // per stored row: O
+};
+
+struct PrefixHead {
+    long long total, share;       // steps (-1: bad offsets), steps per CTA
+};
+struct PrefixEntry {
+    long long step0, row0;        // steps and stored rows before it
+    long long first;              // its first token
+    int tokens, len, units;       // units: tiles of slots = steps per item
+    int blocks;                   // row blocks per KV head (pairs of 128 rows, or one block whose tiles alternate)
+};
+
+template <int DIM>
+struct PrefixShape {
+    static constexpr int SLOTS = DIM == 256 ? 64 : 128;         // per tile
+    static constexpr int SETS = DIM == 256 ? 1 : 2;             // row blocks in work
+    static constexpr int HALVES = DIM / 64;                     // 64-channel parts of 128 bytes per row
+    static constexpr int TILE = SLOTS * DIM * 2, QBLOCK = 128 * DIM * 2;
+    static constexpr int RING = DIM == 64 ? 10 : 5;
+    static constexpr int THREADS = SETS * 128 + 64;
+    static constexpr uint32_t O_COL = 256;                      // S at columns 0 and 128, O from here on
+    static constexpr int BARS = 2 + 2 * RING + 6;
+    static constexpr size_t SMEM = (size_t)SETS * QBLOCK + (size_t)RING * TILE + BARS * 8 + 16 + 64 * 8 + 1024;
+    static constexpr int STORE = SETS * 128;                    // stored rows of a piece at most
+};
+
+// weights of fp16 caches are taken 2^4 larger, to use more of that type's range
+template <typename T>
+constexpr float kWeightBias = 0.0f;
+template <>
+constexpr float kWeightBias<__half> = 4.0f;
+
+constexpr float kLazyRise = 8.0f;                               // powers of two
+
+// ---- entries ----
+
+template <int DIM>
+__device__ __forceinline__ PrefixEntry prefix_entry(const PrefixArgs& a, int e, int32_t& bits) {
+    using Shape = PrefixShape<DIM>;
+    PrefixEntry r;
+    const int P = a.prefix.seqs;
+    long long lo, hi;
+    int len, most;
+    if (e < P) {
+        int s0 = 0, s1 = a.seqs;
+        if (a.seq_offsets != nullptr) {
+            s0 = a.seq_offsets[e];
+            s1 = a.seq_offsets[e + 1];
+            if (s0 < 0 || s1 < s0 || s1 > a.seqs) {
+                bits |= kStatusArg;
+                s0 = s1 = 0;
+            }
+        }
+        lo = a.row_offsets[s0];
+        hi = a.row_offsets[s1];
+        len = a.prefix_lengths[e];
+        most = a.max_prefix;
+    } else {
+        lo = a.row_offsets[e - P];
+        hi = a.row_offsets[e - P + 1];
+        len = a.lengths[e - P];
+        most = a.max_own;
+    }
+    if (lo < 0 || hi < lo) {
+        bits |= kStatusArg;
+        lo = hi = 0;
+    }
+    if (hi > a.rows) {
+        bits |= kStatusCapacity;
+        hi = a.rows;
+        lo = min(lo, hi);
+    }
+    if (len > most) {
+        bits |= kStatusCapacity;
+        len = most;
+    }
+    r.first = lo;
+    r.tokens = (int)(hi - lo);
+    r.len = max(len, 0);
+    r.units = (r.len + Shape::SLOTS - 1) / Shape::SLOTS;
+    const int per = r.tokens <= a.block_tokens ? a.block_tokens : Shape::SETS * a.block_tokens;
+    r.blocks = (r.tokens + per - 1) / per;
+    r.step0 = r.row0 = 0;
+    return r;
+}
+// two sets take alternate tiles of one block of rows
+template <int DIM>
+__device__ __forceinline__ bool alternates(const PrefixArgs& a, const PrefixEntry& e) { return PrefixShape<DIM>::SETS == 1 || e.tokens <= a.block_tokens; }
+// how often a row of the entry is stored per piece
+template <int DIM>
+__device__ __forceinline__ int stored(const PrefixArgs& a, const PrefixEntry& e) { return PrefixShape<DIM>::SETS == 2 && e.tokens <= a.block_tokens ? 2 : 1; }
+__device__ __forceinline__ long long steps_of(const PrefixArgs& a, const PrefixEntry& e) { return (long long)a.prefix.heads * e.blocks * e.units; }
+template <int DIM>
+__device__ __forceinline__ long long rows_of(const PrefixArgs& a, const PrefixEntry& e) {
+    return e.units ? (long long)a.q_heads * e.tokens * stored<DIM>(a, e) : 0;
+}
+
+__device__ __forceinline__ long long warp_scan(long long v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const long long u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+
+// A CTA's pieces, one after the other; every warp walks them for itself.
+template <int DIM>
+struct PieceWalk {
+    PrefixEntry e;
+    int at;                                                     // entry
+    long long step, end;
+    int item, head, block, u0, u1;
+    __device__ __forceinline__ bool next(const PrefixArgs& a) {
+        if (step >= end) return false;
+        int32_t bits = 0;
+        while (step >= e.step0 + steps_of(a, e)) {
+            const long long s = e.step0 + steps_of(a, e), r = e.row0 + rows_of<DIM>(a, e);
+            e = prefix_entry<DIM>(a, ++at, bits);
+            e.step0 = s;
+            e.row0 = r;
+        }
+        const long long in = step - e.step0;
+        item = (int)(in / e.units);
+        u0 = (int)(in - (long long)item * e.units);
+        u1 = (int)min((long long)e.units, u0 + (end - step));
+        step += u1 - u0;
+        head = item / e.blocks;
+        block = item - head * e.blocks;
+        if (is_own(a)) {
+            // tiles behind the last slot that the block's last token sees hold nothing for it
+            const int per = (alternates<DIM>(a, e) ? 1 : 2) * a.block_tokens, last = min(e.tokens, (block + 1) * per);
+            const int seen = max(0, e.len - e.tokens + last);
+            u1 = max(u0, min(u1, (seen + PrefixShape<DIM>::SLOTS - 1) / PrefixShape<DIM>::SLOTS));
+        }
+        return true;
+    }
+    __device__ __forceinline__ bool is_own(const PrefixArgs& a) const { return at >= a.prefix.seqs; }
+    __device__ __forceinline__ int tiles() const { return u1 - u0; }
+    __device__ __forceinline__ bool pair(const PrefixArgs& a) const { return !alternates<DIM>(a, e); }
+    // first stored row
+    __device__ __forceinline__ long long store(const PrefixArgs& a) const {
+        const long long per_head = (long long)e.tokens * a.group * stored<DIM>(a, e);
+        return (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + head * per_head + (long long)block * (pair(a) ? 2 : 1) * a.block_tokens * a.group;
+    }
+};
+
+// ---- products ----
+
+// instruction descriptor of tcgen05.mma kind::f16 with M = 128 (see kTcIdesc): type of A and B, N, B with its N axis contiguous
+template <typename T>
+__host__ __device__ constexpr uint32_t attend_idesc(int n, bool b_by_n) {
+    const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)b_by_n << 16) | ((uint32_t)(n / 8) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// A in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Operand whose row axis (channels) is contiguous, 128-byte swizzle: groups of eight slots 1024 bytes apart, 64-channel
+// parts `part` bytes apart.
+__device__ __forceinline__ uint64_t operand_by_n(uint32_t addr, uint32_t part) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(part >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+          "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+          "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]),
+          "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]),
+          "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void copy_queries(uint32_t dst, const CUtensorMap* map, int head, int half, int row, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(head), "r"(half), "r"(row), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void copy_slots(uint32_t dst, const CUtensorMap* map, int place, int half, int head, int page, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(place), "r"(half), "r"(head), "r"(page), "r"(bar)
+        : "memory");
+}
+
+struct PrefixMaps {
+    CUtensorMap q, k[2], v[2];    // prefix, own
+};
+
+template <typename T, int DIM>
+__global__ void __launch_bounds__(PrefixShape<DIM>::THREADS, 1)
+k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ PrefixMaps maps) {
+    using Shape = PrefixShape<DIM>;
+    constexpr int SLOTS = Shape::SLOTS, SETS = Shape::SETS, HALVES = Shape::HALVES, RING = Shape::RING, TILE = Shape::TILE;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t qmem = smem_u32(smem), ring = qmem + SETS * Shape::QBLOCK;
+    unsigned char* rest = smem + SETS * Shape::QBLOCK + RING * TILE;
+    const uint32_t q_full = smem_u32(rest), q_empty = q_full + 8, full = q_full + 16, empty = full + 8 * RING;
+    const uint32_t s_full = empty + 8 * RING, p_full = s_full + 16, o_full = p_full + 16;
+    uint32_t* tmem_word = reinterpret_cast<uint32_t*>(rest + Shape::BARS * 8);
+    long long* scan = reinterpret_cast<long long*>(rest + Shape::BARS * 8 + 16);        // [64]
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    constexpr int COPY_WARP = SETS * 4, MMA_WARP = COPY_WARP + 1, WARPS = MMA_WARP + 1;
+    if (tid == 0) {
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        for (int s = 0; s < RING; s++) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; b++) {
+            mbar_init(s_full + 8 * b, 1);
+            mbar_init(p_full + 8 * b, 4);
+            mbar_init(o_full + 8 * b, 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_word)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_word);
+    wait_for_prior_kernel();
+    let_next_kernel_start();
+
+    // ---- shares: the sum of all entries' steps, then the entry in which this CTA's first step lies ----
+    const int entries = a.prefix.seqs + a.own.seqs;
+    int32_t bits = 0;
+    long long mine = 0;
+    for (int e = tid; e < entries; e += Shape::THREADS) {
+        const PrefixEntry x = prefix_entry<DIM>(a, e, bits);
+        mine += steps_of(a, x);
+    }
+    mine = warp_scan(mine, lane);
+    if (lane == 31) scan[warp] = mine;
+    const int bad = __syncthreads_or(bits & kStatusArg);
+    if (blockIdx.x == 0 && bits) raise_status(a.status, bits);
+    long long total = 0;
+    for (int w = 0; w < WARPS; w++) total += scan[w];
+    if (bad) total = 0;
+    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    if (blockIdx.x == 0 && tid == 0) *a.head = PrefixHead{bad ? -1 : total, share};
+    PieceWalk<DIM> walk;
+    walk.step = min(total, (long long)blockIdx.x * share);
+    walk.end = min(total, walk.step + share);
+    if (walk.step < walk.end) {
+        long long steps = 0, rows = 0;                          // before the entries of this go
+        PrefixEntry* found = reinterpret_cast<PrefixEntry*>(scan + 40);
+        int* found_at = reinterpret_cast<int*>(scan + 48);
+        for (int e0 = 0; e0 < entries; e0 += Shape::THREADS) {
+            const int e = e0 + tid;
+            PrefixEntry x = {};
+            long long s = 0, r = 0;
+            if (e < entries) {
+                x = prefix_entry<DIM>(a, e, bits);
+                s = steps_of(a, x);
+                r = rows_of<DIM>(a, x);
+            }
+            const long long si = warp_scan(s, lane), ri = warp_scan(r, lane);
+            __syncthreads();
+            if (lane == 31) {
+                scan[warp] = si;
+                scan[16 + warp] = ri;
+            }
+            __syncthreads();
+            x.step0 = steps + si - s;
+            x.row0 = rows + ri - r;
+            for (int w = 0; w < WARPS; w++) {
+                if (w < warp) {
+                    x.step0 += scan[w];
+                    x.row0 += scan[16 + w];
+                }
+                steps += scan[w];
+                rows += scan[16 + w];
+            }
+            if (e < entries && s > 0 && x.step0 <= walk.step && walk.step < x.step0 + s) {
+                *found = x;
+                *found_at = e;
+            }
+            if (blockIdx.x == 0 && e < entries) a.entries[e] = x;
+            if (blockIdx.x != 0 && steps > walk.step) break;    // (the same for the whole CTA)
+        }
+        __syncthreads();
+        walk.e = *found;
+        walk.at = *found_at;
+    }
+
+    bool timed_out = false;
+    if (warp == COPY_WARP) {
+        // ------------------------------------- copies -------------------------------------
+        int n = 0, p = 0;                                       // ring slots and pieces taken up so far
+        while (!timed_out && walk.next(a)) {
+            if (walk.tiles() == 0) continue;
+            const bool pair = walk.pair(a);
+            const int own = walk.is_own(a), sets = pair ? 2 : 1;
+            const CacheView& c = own ? a.own : a.prefix;
+            const int box = a.page_box[own], boxes = SLOTS / box, row = own ? walk.at - a.prefix.seqs : walk.at;
+            if (p > 0 && !mbar_wait(q_empty, p - 1, timed_out)) break;
+            if (lane == 0) {
+                const int bytes = a.block_tokens * a.group * 128;
+                mbar_expect_tx(q_full, sets * HALVES * bytes);
+                for (int t = 0; t < sets; t++)
+                    for (int h = 0; h < HALVES; h++)
+                        copy_queries(qmem + t * Shape::QBLOCK + h * (128 * 128), &maps.q, walk.head * a.group, h,
+                                     (int)(walk.e.first + (long long)(walk.block * sets + t) * a.block_tokens), q_full);
+            }
+            p++;
+            __syncwarp();
+            auto load = [&](int tile, bool values) -> bool {
+                int page = 0, place = 0;
+                if (lane < boxes) {
+                    const int slot = (walk.u0 + tile) * SLOTS + lane * box, stretch = slot / c.page;
+                    place = slot - stretch * c.page;
+                    page = (int)c.pages;                        // beyond the pool: zeros
+                    if (slot < walk.e.len) {
+                        const int pg = c.table[row * c.table_stride + stretch];
+                        if (pg >= 0 && pg < c.pages) page = pg;
+                        else raise_status(a.status, kStatusArg);
+                    }
+                }
+                const int s = n % RING;
+                if (n >= RING && !mbar_wait(empty + 8 * s, n / RING - 1, timed_out)) return false;
+                if (lane == 0) mbar_expect_tx(full + 8 * s, TILE);
+                __syncwarp();
+                if (lane < boxes) {
+                    const CUtensorMap* map = values ? &maps.v[own] : &maps.k[own];
+#pragma unroll
+                    for (int h = 0; h < HALVES; h++)
+                        copy_slots(ring + s * TILE + h * (SLOTS * 128) + lane * box * 128, map, place, h, walk.head, page, full + 8 * s);
+                }
+                n++;
+                __syncwarp();
+                return true;
+            };
+            // in the order of the products: see there
+            const int tiles = walk.tiles();
+            if (!load(0, false)) break;
+            if (!pair && tiles > 1 && !load(1, false)) break;
+            for (int j = 0; j < tiles; j++) {
+                if (!load(j, true)) break;
+                const int ahead = j + (pair ? 1 : 2);
+                if (ahead < tiles && !load(ahead, false)) break;
+            }
+        }
+        // the CTA must not end with copies in flight
+        for (int i = max(0, n - RING); i < n; i++) {
+            bool late = false;
+            mbar_wait_sleep(full + 8 * (i % RING), i / RING, late);
+            timed_out |= late;
+        }
+        if (p > 0) {
+            bool late = false;
+            mbar_wait_sleep(q_full, p - 1, late);
+            timed_out |= late;
+        }
+    } else if (warp == MMA_WARP) {
+        // ------------------------------------- products -------------------------------------
+        // Step x of a piece: tile x / 2 for set x % 2, or tile x where tiles alternate.  First the logits of steps 0 and 1, then the
+        // values of step x and the logits of step x + 2: those of one set run while the other's exponentials are formed.
+        int n = 0, p = 0, uses[2] = {0, 0};                     // ring slots, pieces, products with either set's weights
+        while (!timed_out && walk.next(a)) {
+            const int tiles = walk.tiles();
+            if (tiles == 0) continue;
+            const bool pair = walk.pair(a);
+            const int steps = pair ? 2 * tiles : tiles;
+            if (!mbar_wait(q_full, p, timed_out)) break;
+            p++;
+            tc_fence_after();
+            // ring slot (counted from the piece's first) of a tile's keys and values
+            auto key_slot = [&](int j) { return pair ? 2 * j : j < 2 ? j : 2 * j - 1; };
+            auto value_slot = [&](int j) { return pair ? 2 * j + 1 : j + 1 < tiles ? 2 * j + 2 : 2 * j + 1; };
+            auto logits = [&](int x) -> bool {
+                const int j = pair ? x >> 1 : x, b = x & 1, set = pair ? b : 0;
+                const int i = n + key_slot(j), s = i % RING;
+                if (!mbar_wait(full + 8 * s, i / RING, timed_out)) return false;
+                tc_fence_after();
+                if (lane == 0) {
+#pragma unroll
+                    for (int k = 0; k < DIM / 16; k++) {
+                        const uint32_t in = (k & 3) * 32;
+                        mma_ss(tmem + b * 128, tc_operand(qmem + set * Shape::QBLOCK + (k >> 2) * (128 * 128) + in),
+                               tc_operand(ring + s * TILE + (k >> 2) * (SLOTS * 128) + in), attend_idesc<T>(SLOTS, false), k > 0);
+                    }
+                    tc_commit(s_full + 8 * b);
+                    if (!pair || b == 1) tc_commit(empty + 8 * s);
+                    if (x + 1 == steps) tc_commit(q_empty);
+                }
+                __syncwarp();
+                return true;
+            };
+            auto values = [&](int x) -> bool {
+                const int j = pair ? x >> 1 : x, b = x & 1, set = SETS == 2 ? b : 0;
+                const int i = n + value_slot(j), s = i % RING;
+                if (!mbar_wait(full + 8 * s, i / RING, timed_out)) return false;
+                const int there = walk.e.len - (walk.u0 + j) * SLOTS;
+                if (there < SLOTS && (!pair || b == 0)) {       // what lies behind the last slot may be anything: 0 times it must be 0
+                    for (int w = lane; w < (SLOTS - there) * 8 * HALVES; w += 32) {
+                        const int h = w / ((SLOTS - there) * 8), u = w - h * (SLOTS - there) * 8;
+                        *reinterpret_cast<uint4*>(smem + SETS * Shape::QBLOCK + s * TILE + h * (SLOTS * 128) + there * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                }
+                if (!mbar_wait(p_full + 8 * b, uses[b]++, timed_out)) return false;
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint32_t d = tmem + Shape::O_COL + set * DIM;
+#pragma unroll
+                    for (int k = 0; k < SLOTS / 16; k++)
+                        mma_ts(d, tmem + b * 128 + k * 8, operand_by_n(ring + s * TILE + k * 2048, SLOTS * 128), attend_idesc<T>(DIM, true),
+                               x >= SETS || k > 0);
+                    tc_commit(o_full + 8 * set);
+                    if (!pair || b == 1) tc_commit(empty + 8 * s);
+                }
+                __syncwarp();
+                return true;
+            };
+            bool ok = logits(0) && (steps < 2 || logits(1));
+            for (int x = 0; ok && x < steps; x++) ok = values(x) && (x + 2 >= steps || logits(x + 2));
+            if (!ok) break;
+            n += 2 * tiles;
+        }
+    } else {
+        // ------------------------------------- softmax -------------------------------------
+        const int set = warp >> 2, row = 32 * (warp & 3) + lane;
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+        const uint32_t o_at = tmem + lanes + Shape::O_COL + set * DIM;
+        const int tok = row / a.group;
+        int s_uses[2] = {0, 0}, o_uses = 0;                     // logits taken from either place, products into O
+        while (!timed_out && walk.next(a)) {
+            const bool pair = walk.pair(a);
+            const int tiles = walk.tiles(), token = (walk.block * (pair ? 2 : 1) + (pair ? set : 0)) * a.block_tokens + tok;
+            const bool there = tok < a.block_tokens && token < walk.e.tokens;
+            // slots that this row sees
+            const int limit = walk.is_own(a) ? min(walk.e.len, walk.e.len - walk.e.tokens + token + 1) : walk.e.len;
+            float m = -INFINITY, l = 0.0f;
+            const int steps = pair ? 2 * tiles : tiles;
+            bool first = true;
+            for (int x = SETS == 2 ? set : 0; x < steps; x += SETS) {
+                const int j = pair ? x >> 1 : x, b = x & 1;
+                const uint32_t s_at = tmem + lanes + b * 128;
+                if (!mbar_wait_warp(s_full + 8 * b, s_uses[b]++, timed_out)) break;
+                tc_fence_after();
+                uint32_t v[SLOTS / 32][32];
+#pragma unroll
+                for (int i = 0; i < SLOTS / 32; i++) tc_load32(s_at + 32 * i, v[i]);
+                const int left = limit - (walk.u0 + j) * SLOTS;  // slots of this tile that the row sees
+                if (__any_sync(0xffffffffu, left < SLOTS)) {
+#pragma unroll
+                    for (int i = 0; i < SLOTS; i++)
+                        if (i >= left) v[i / 32][i % 32] = 0xff800000u;
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < SLOTS; i++) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i / 32][i % 32]));
+                const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                const bool rise = (tile_top - m) * a.scale_log2 > kLazyRise;     // (not for -inf after -inf)
+                float factor = 1.0f;
+                if (rise) {
+                    factor = exp2_fast((m - tile_top) * a.scale_log2);
+                    m = tile_top;
+                }
+                if (!first && __any_sync(0xffffffffu, rise)) {
+                    if (!mbar_wait_warp(o_full + 8 * set, o_uses - 1, timed_out)) break;
+                    tc_fence_after();
+                    l *= factor;
+#pragma unroll 1
+                    for (int i = 0; i < DIM; i += 32) {
+                        uint32_t o[32];
+                        tc_load32(o_at + i, o);
+#pragma unroll
+                        for (int k = 0; k < 32; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
+                        tmem_store32(o_at + i, o);
+                    }
+                }
+                first = false;
+                const float base = m == -INFINITY ? 0.0f : kWeightBias<T> - m * a.scale_log2;
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < SLOTS / 32; i++) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int k = 0; k < 16; k++) {
+                        const float p0 = exp2_fast(fmaf(__uint_as_float(v[i][2 * k]), a.scale_log2, base));
+                        const float p1 = exp2_fast(fmaf(__uint_as_float(v[i][2 * k + 1]), a.scale_log2, base));
+                        sum[2 * (k & 1)] += p0;
+                        sum[2 * (k & 1) + 1] += p1;
+                        w[k] = Pair<T>::pack(p0, p1);
+                    }
+                    tmem_store16(s_at + 16 * i, w);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_wait_store();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 8 * b);
+                o_uses++;
+            }
+            if (timed_out) break;
+            // this piece's O, l and m
+            const long long store = walk.store(a) + (SETS == 2 ? (pair ? (long long)set * a.block_tokens : (long long)set * walk.e.tokens) : 0) * a.group + row;
+            if (!first) {
+                if (!mbar_wait_warp(o_full + 8 * set, o_uses - 1, timed_out)) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int i = 0; i < DIM; i += 32) {
+                    uint32_t o[32];
+                    tc_load32(o_at + i, o);
+                    if (there) {
+                        float4* to = reinterpret_cast<float4*>(a.partial + store * DIM + i);
+#pragma unroll
+                        for (int k = 0; k < 8; k++)
+                            to[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+                    }
+                }
+                tc_fence_before();
+            }
+            if (there) a.stats[store] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == MMA_WARP) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+    if (timed_out) raise_status(a.status, kStatusWaitTimeout);
+}
+
+// ---- pieces of a row to its output ----
+
+constexpr int kPrefixJoinThreads = 128;
+
+// One warp per (token, query head).
+template <typename T, int DIM>
+__global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid_constant__ PrefixArgs a) {
+    constexpr int PER = DIM / 32;                               // channels per lane
+    const int lane = threadIdx.x & 31;
+    wait_for_prior_kernel();
+    let_next_kernel_start();
+    const long long w = ((long long)blockIdx.x * kPrefixJoinThreads + threadIdx.x) >> 5;
+    const long long token = w / a.q_heads;
+    const int qh = (int)(w - token * a.q_heads);
+    if (token >= a.rows || token < a.row_offsets[0] || token >= a.row_offsets[a.seqs]) return;
+    const PrefixHead head = *a.head;
+    if (head.total < 0) return;
+    const int seq = sequence_of(a.row_offsets, a.seqs, token, lane);
+    int of[2] = {0, a.own.seqs > 0 ? a.prefix.seqs + seq : -1};
+    if (a.seq_offsets != nullptr)
+        of[0] = seq < a.seq_offsets[0] || seq >= a.seq_offsets[a.prefix.seqs] ? -1 : sequence_of(a.seq_offsets, a.prefix.seqs, seq, lane);
+    const int kv = qh / a.group, g = qh - kv * a.group;
+    float top = -INFINITY, total = 0.0f, acc[PER];
+#pragma unroll
+    for (int i = 0; i < PER; i++) acc[i] = 0.0f;
+    for (int which = 0; which < 2; which++) {
+        if (of[which] < 0 || head.share == 0) continue;
+        const PrefixEntry e = a.entries[of[which]];
+        if (e.units == 0 || e.tokens == 0) continue;
+        if (token < e.first || token >= e.first + e.tokens) continue;      // (offsets that go up and down)
+        const int in = (int)(token - e.first), copies = stored<DIM>(a, e);
+        const int per = alternates<DIM>(a, e) ? a.block_tokens : 2 * a.block_tokens;
+        const int block = in / per;
+        const long long s0 = e.step0 + ((long long)kv * e.blocks + block) * e.units;
+        const long long c0 = s0 / head.share, c1 = (s0 + e.units - 1) / head.share;
+        const long long at = e.row0 + (long long)kv * e.tokens * a.group * copies + (long long)in * a.group + g;
+        const int parts = (int)(c1 - c0 + 1) * copies;
+        for (int i0 = 0; i0 < parts; i0 += 32) {
+            // a lane looks after one piece's m and l
+            const int i = i0 + lane;
+            long long row = 0;
+            float2 s = make_float2(-INFINITY, 0.0f);
+            if (i < parts) {
+                row = (c0 + i / copies) * PrefixShape<DIM>::STORE + at + (long long)(i % copies) * e.tokens * a.group;
+                s = a.stats[row];
+            }
+            float most = s.x;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            const float now = fmaxf(top, most), keep = top == -INFINITY ? 0.0f : exp2f(top - now);
+            const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - now);
+            top = now;
+            total *= keep;
+#pragma unroll
+            for (int k = 0; k < PER; k++) acc[k] *= keep;
+            float sum = weight * s.y;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            total += sum;
+            const int n = min(32, parts - i0);
+            for (int k = 0; k < n; k++) {
+                const float f = __shfl_sync(0xffffffffu, weight, k);
+                const long long r = __shfl_sync(0xffffffffu, row, k);
+                if (f == 0.0f) continue;                        // (a piece without tiles stored no O)
+                const float* from = a.partial + r * DIM + lane * PER;
+#pragma unroll
+                for (int c = 0; c < PER; c++) acc[c] += f * from[c];
+            }
+        }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (token * a.q_heads + qh) * DIM + lane * PER);
+#pragma unroll
+    for (int c = 0; c < PER; c += 2) to[c / 2] = Pair<T>::pack(acc[c] * inv, acc[c + 1] * inv);
+    if (a.lse != nullptr && lane == 0) a.lse[token * a.q_heads + qh] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+}
+
+}  // namespace sttm

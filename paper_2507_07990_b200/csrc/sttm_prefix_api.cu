@@ -1,0 +1,142 @@
+// Host side of sttm_prefix_attend: argument checks, workspace layout, launches.
+#include "../../include/sttm.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "sttm_cache_host.cuh"
+#include "sttm_prefix.cuh"
+
+namespace {
+
+using namespace sttm;
+
+struct PrefixPlan {
+    long long grid, join_grid;
+    size_t entries, stats, partial, total;      // byte offsets in the workspace, and its size
+};
+
+sttm_status plan_prefix(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p, PrefixPlan* pl) {
+    sttm_status s = check_cache(prefix);
+    if (s != STTM_OK) return s;
+    if (own != nullptr && (s = check_cache(own)) != STTM_OK) return s;
+    if (p == nullptr || p->rows < 0 || p->seqs < 1 || p->q_heads < 1 || p->q_heads % prefix->heads != 0) return STTM_ERR_ARG;
+    if (own != nullptr && (own->heads != prefix->heads || own->dim != prefix->dim || own->dtype != prefix->dtype || own->seqs != p->seqs))
+        return STTM_ERR_ARG;
+    if (p->seq_offsets == nullptr && prefix->seqs != 1) return STTM_ERR_ARG;
+    if (p->max_prefix < 1 || (long long)p->max_prefix > (long long)prefix->table_width * prefix->page) return STTM_ERR_ARG;
+    if (own != nullptr && (p->max_own < 1 || (long long)p->max_own > (long long)own->table_width * own->page)) return STTM_ERR_ARG;
+    const int group = p->q_heads / prefix->heads;
+    if (group > 64 || p->max_prefix > kMaxSlots || (own != nullptr && p->max_own > kMaxSlots)) return STTM_ERR_UNSUPPORTED;
+    if (p->rows > INT_MAX - 256 || p->seqs > INT_MAX / 2 || prefix->seqs > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
+    pl->grid = sm_count();
+    const long long heads = p->rows * p->q_heads;
+    pl->join_grid = (heads + kPrefixJoinThreads / 32 - 1) / (kPrefixJoinThreads / 32);
+    if (pl->join_grid > INT_MAX) return STTM_ERR_UNSUPPORTED;
+    // every row is stored twice at most per kind of entry, and every CTA's pieces start a fresh stretch
+    const long long rows = pl->grid * 256 + heads * (own != nullptr ? 4 : 2);
+    pl->entries = 256;
+    pl->stats = pl->entries + align_up(((size_t)prefix->seqs + (own != nullptr ? own->seqs : 0)) * sizeof(PrefixEntry));
+    pl->partial = pl->stats + align_up((size_t)rows * sizeof(float2));
+    pl->total = pl->partial + align_up((size_t)rows * prefix->dim * 4);
+    return STTM_OK;
+}
+
+// Keys (or values) as [page][head][64-channel part][slot][64 channels], a copy taking `box` slots of one part: rows of 128
+// bytes under the 128-byte swizzle.
+sttm_status make_part_map(const sttm_cache* c, void* base, int box, CUtensorMap* map) {
+    const EncodeTiledFn encode = tensor_map_encoder();
+    if (encode == nullptr) return STTM_ERR_CUDA;
+    const cuuint64_t inner = (cuuint64_t)c->slot_stride * 2;
+    const cuuint64_t dims[5] = {64, (cuuint64_t)c->page, (cuuint64_t)(c->dim / 64), (cuuint64_t)c->heads, (cuuint64_t)c->pages};
+    const cuuint64_t strides[4] = {inner, 128, c->heads > 1 ? (cuuint64_t)c->head_stride * 2 : inner,
+                                   c->pages > 1 ? (cuuint64_t)c->page_stride * 2 : inner};
+    const cuuint32_t shape[5] = {64, (cuuint32_t)box, 1, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
+    const CUresult r = encode(map, c->dtype == STTM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
+                              base, dims, strides, shape, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? STTM_OK : STTM_ERR_UNSUPPORTED;
+}
+
+// Queries as [row][64-channel part][head][64 channels], a copy taking one part of `tokens` rows' heads of one KV head.
+sttm_status make_query_map(const sttm_cache* c, const sttm_prefix_params* p, int group, int tokens, CUtensorMap* map) {
+    const EncodeTiledFn encode = tensor_map_encoder();
+    if (encode == nullptr) return STTM_ERR_CUDA;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)p->q_heads, (cuuint64_t)(c->dim / 64), (cuuint64_t)p->rows};
+    const cuuint64_t head = p->q_heads > 1 ? (cuuint64_t)p->q_head * 2 : 128;
+    const cuuint64_t strides[3] = {head, 128, p->rows > 1 ? (cuuint64_t)p->q_row * 2 : head};
+    const cuuint32_t box[4] = {64, (cuuint32_t)group, 1, (cuuint32_t)tokens}, ones[4] = {1, 1, 1, 1};
+    const CUresult r = encode(map, c->dtype == STTM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                              const_cast<void*>(p->q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? STTM_OK : STTM_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sttm_prefix_workspace_bytes(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p) {
+    PrefixPlan pl;
+    return plan_prefix(prefix, own, p, &pl) == STTM_OK ? pl.total : 0;
+}
+
+sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p, void* ws, size_t ws_bytes,
+                               void* stream) {
+    PrefixPlan pl;
+    sttm_status s = plan_prefix(prefix, own, p, &pl);
+    if (s != STTM_OK) return s;
+    if (p->row_offsets == nullptr || p->prefix_lengths == nullptr || (own != nullptr && p->lengths == nullptr) || ws == nullptr) return STTM_ERR_ARG;
+    if (misaligned(p->row_offsets, 8) || odd_address(p->seq_offsets, p->prefix_lengths, p->lengths, p->lse, p->device_status) || misaligned(ws, 256))
+        return STTM_ERR_ARG;
+    if (!std::isfinite(p->scale) || !(p->scale > 0.0f)) return STTM_ERR_ARG;
+    if (p->rows > 0) {
+        if (p->q == nullptr || p->out == nullptr || misaligned(p->q, 16) || misaligned(p->out, 16)) return STTM_ERR_ARG;
+        if ((p->rows > 1 && (!multiple_of_8(p->q_row) || p->q_row < prefix->dim)) ||
+            (p->q_heads > 1 && (!multiple_of_8(p->q_head) || p->q_head < prefix->dim)))
+            return STTM_ERR_ARG;
+    }
+    if (ws_bytes < pl.total) return STTM_ERR_WORKSPACE;
+    if (p->rows == 0) return STTM_OK;
+    char* w = (char*)ws;
+    PrefixArgs a = {};
+    a.prefix = view_of(prefix);
+    a.own = own != nullptr ? view_of(own) : CacheView{};
+    a.rows = p->rows;
+    a.q_heads = p->q_heads;
+    a.group = p->q_heads / prefix->heads;
+    a.block_tokens = 128 / a.group;
+    a.seqs = p->seqs;
+    a.row_offsets = (const long long*)p->row_offsets;
+    a.seq_offsets = p->seq_offsets;
+    a.prefix_lengths = p->prefix_lengths;
+    a.lengths = p->lengths;
+    a.max_prefix = p->max_prefix;
+    a.max_own = p->max_own;
+    a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
+    a.out = (uint16_t*)p->out;
+    a.lse = p->lse;
+    a.status = p->device_status;
+    a.head = (PrefixHead*)w;
+    a.entries = (PrefixEntry*)(w + pl.entries);
+    a.stats = (float2*)(w + pl.stats);
+    a.partial = (float*)(w + pl.partial);
+    return by_type(prefix, [&](auto tag, auto dim) -> sttm_status {
+        using T = decltype(tag);
+        constexpr int D = decltype(dim)::value;
+        PrefixMaps maps;
+        sttm_status r = make_query_map(prefix, p, a.group, a.block_tokens, &maps.q);
+        for (int i = 0; i < 2 && r == STTM_OK; i++) {
+            const sttm_cache* c = i && own != nullptr ? own : prefix;
+            a.page_box[i] = std::min(c->page & -c->page, PrefixShape<D>::SLOTS);
+            if ((r = make_part_map(c, c->k, a.page_box[i], &maps.k[i])) == STTM_OK) r = make_part_map(c, c->v, a.page_box[i], &maps.v[i]);
+        }
+        if (r != STTM_OK) return r;
+        static size_t allowed[kMaxDevices] = {};
+        if ((r = allow_smem((const void*)k_prefix_attend<T, D>, PrefixShape<D>::SMEM, allowed)) != STTM_OK) return r;
+        if ((r = launch(k_prefix_attend<T, D>, pl.grid, PrefixShape<D>::THREADS, PrefixShape<D>::SMEM, 0, stream, a, maps)) != STTM_OK) return r;
+        return launch(k_prefix_join<T, D>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a);
+    });
+}
+
+}  // extern "C"
