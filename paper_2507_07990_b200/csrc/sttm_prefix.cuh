@@ -14,9 +14,10 @@
 // that issues the products.  256-channel heads fill tensor memory with one O: there one block's tiles alternate between two
 // places for S.
 //
-// Work is cut into equal shares of tiles over all CTAs whatever the lengths are (which the host does not know): entries are the prefixes
-// and then the sequences' own slots; an entry has an item per KV head and block of rows, an item as many steps as tiles of
-// slots.  What a CTA has of an item is a piece: O, l and m of its rows go to memory, and k_prefix_join puts a row's pieces together.
+// Work is cut into equal shares of steps over all CTAs whatever the lengths are (which the host does not know): entries are the prefixes
+// and then the sequences' own slots; an entry has an item per KV head and block of rows, an item a step per tile of slots and
+// kPieceSteps for what it costs besides (queries in, O out).  What a CTA has of an item is a piece: O, l and m of its rows go to
+// memory, and k_prefix_join puts a row's pieces together.
 #pragma once
 
 #include "sttm_cache.cuh"
@@ -50,7 +51,7 @@ struct PrefixHead {
 struct PrefixEntry {
     long long step0, row0;        // steps and stored rows before it
     long long first;              // its first token
-    int tokens, len, units;       // units: tiles of slots = steps per item
+    int tokens, len, units;       // units: steps per item
     int blocks;                   // row blocks per KV head (pairs of 128 rows, or one block whose tiles alternate)
 };
 
@@ -61,10 +62,10 @@ struct PrefixShape {
     static constexpr int HALVES = DIM / 64;                     // 64-channel parts of 128 bytes per row
     static constexpr int TILE = SLOTS * DIM * 2, QBLOCK = 128 * DIM * 2;
     static constexpr int RING = DIM == 64 ? 10 : 5;
-    static constexpr int THREADS = SETS * 128 + 64;
+    static constexpr int THREADS = SETS == 2 ? 384 : 192;       // softmax warps, the two others (and two idle ones: see the register split)
     static constexpr uint32_t O_COL = 256;                      // S at columns 0 and 128, O from here on
     static constexpr int BARS = 2 + 2 * RING + 6;
-    static constexpr size_t SMEM = (size_t)SETS * QBLOCK + (size_t)RING * TILE + BARS * 8 + 16 + 64 * 8 + 1024;
+    static constexpr size_t SMEM = (size_t)SETS * QBLOCK + (size_t)RING * TILE + BARS * 8 + 16 + 64 * 8 + 128 * 8 + 1024;
     static constexpr int STORE = SETS * 128;                    // stored rows of a piece at most
 };
 
@@ -75,6 +76,7 @@ template <>
 constexpr float kWeightBias<__half> = 4.0f;
 
 constexpr float kLazyRise = 8.0f;                               // powers of two
+constexpr int kPieceSteps = 3;
 
 // ---- entries ----
 
@@ -121,7 +123,7 @@ __device__ __forceinline__ PrefixEntry prefix_entry(const PrefixArgs& a, int e, 
     r.first = lo;
     r.tokens = (int)(hi - lo);
     r.len = max(len, 0);
-    r.units = (r.len + Shape::SLOTS - 1) / Shape::SLOTS;
+    r.units = r.len > 0 ? (r.len + Shape::SLOTS - 1) / Shape::SLOTS + kPieceSteps : 0;
     const int per = r.tokens <= a.block_tokens ? a.block_tokens : Shape::SETS * a.block_tokens;
     r.blocks = (r.tokens + per - 1) / per;
     r.step0 = r.row0 = 0;
@@ -130,14 +132,8 @@ __device__ __forceinline__ PrefixEntry prefix_entry(const PrefixArgs& a, int e, 
 // two sets take alternate tiles of one block of rows
 template <int DIM>
 __device__ __forceinline__ bool alternates(const PrefixArgs& a, const PrefixEntry& e) { return PrefixShape<DIM>::SETS == 1 || e.tokens <= a.block_tokens; }
-// how often a row of the entry is stored per piece
-template <int DIM>
-__device__ __forceinline__ int stored(const PrefixArgs& a, const PrefixEntry& e) { return PrefixShape<DIM>::SETS == 2 && e.tokens <= a.block_tokens ? 2 : 1; }
 __device__ __forceinline__ long long steps_of(const PrefixArgs& a, const PrefixEntry& e) { return (long long)a.prefix.heads * e.blocks * e.units; }
-template <int DIM>
-__device__ __forceinline__ long long rows_of(const PrefixArgs& a, const PrefixEntry& e) {
-    return e.units ? (long long)a.q_heads * e.tokens * stored<DIM>(a, e) : 0;
-}
+__device__ __forceinline__ long long rows_of(const PrefixArgs& a, const PrefixEntry& e) { return e.units ? (long long)a.q_heads * e.tokens : 0; }
 
 __device__ __forceinline__ long long warp_scan(long long v, int lane) {
 #pragma unroll
@@ -159,16 +155,17 @@ struct PieceWalk {
         if (step >= end) return false;
         int32_t bits = 0;
         while (step >= e.step0 + steps_of(a, e)) {
-            const long long s = e.step0 + steps_of(a, e), r = e.row0 + rows_of<DIM>(a, e);
+            const long long s = e.step0 + steps_of(a, e), r = e.row0 + rows_of(a, e);
             e = prefix_entry<DIM>(a, ++at, bits);
             e.step0 = s;
             e.row0 = r;
         }
         const long long in = step - e.step0;
         item = (int)(in / e.units);
-        u0 = (int)(in - (long long)item * e.units);
-        u1 = (int)min((long long)e.units, u0 + (end - step));
-        step += u1 - u0;
+        const int from = (int)(in - (long long)item * e.units), to = (int)min((long long)e.units, from + (end - step));
+        step += to - from;
+        u0 = max(0, from - kPieceSteps);
+        u1 = max(0, to - kPieceSteps);
         head = item / e.blocks;
         block = item - head * e.blocks;
         if (is_own(a)) {
@@ -184,8 +181,7 @@ struct PieceWalk {
     __device__ __forceinline__ bool pair(const PrefixArgs& a) const { return !alternates<DIM>(a, e); }
     // first stored row
     __device__ __forceinline__ long long store(const PrefixArgs& a) const {
-        const long long per_head = (long long)e.tokens * a.group * stored<DIM>(a, e);
-        return (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + head * per_head + (long long)block * (pair(a) ? 2 : 1) * a.block_tokens * a.group;
+        return (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + ((long long)head * e.tokens + (long long)block * (pair(a) ? 2 : 1) * a.block_tokens) * a.group;
     }
 };
 
@@ -237,6 +233,66 @@ __device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&v)
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// loads of 32 columns that are on their way until tmem_wait_load; what they bring is used after tmem_loaded
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]));
+}
+// two numbers at a time
+__device__ __forceinline__ uint64_t both(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void apart(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// the largest of three; NaN if one is
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+// 2^x twice without the special-function unit, for x in [-126, 127) (below: 2^-126): x = n + f with |f| <= 1/2, 2^f by the polynomial
+// of degree 4 whose largest relative error is least (2.6e-6: Remez exchange over [-1/2, 1/2]), n added to the exponent.
+__device__ __forceinline__ void exp2_pair(uint64_t x, float& x0, float& x1) {
+    apart(x, x0, x1);
+    x = both(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
+    const uint64_t shift = both(12582912.0f, 12582912.0f);      // 1.5 * 2^23: the sum's lowest bits are n
+    const uint64_t t = add2(x, shift), n = add2(t, both(-12582912.0f, -12582912.0f));
+    const uint64_t f = fma2(n, both(-1.0f, -1.0f), x);
+    uint64_t p = fma2(both(0.009570102f, 0.009570102f), f, both(0.05591786f, 0.05591786f));
+    p = fma2(p, f, both(0.24024744f, 0.24024744f));
+    p = fma2(p, f, both(0.6931218f, 0.6931218f));
+    p = fma2(p, f, both(0.9999993f, 0.9999993f));
+    float t0, t1;
+    apart(t, t0, t1);
+    apart(p, x0, x1);
+    x0 = __uint_as_float(__float_as_uint(x0) + (__float_as_uint(t0) << 23));
+    x1 = __uint_as_float(__float_as_uint(x1) + (__float_as_uint(t1) << 23));
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -256,6 +312,11 @@ __device__ __forceinline__ void copy_slots(uint32_t dst, const CUtensorMap* map,
         : "memory");
 }
 
+__device__ __forceinline__ void store32(float* to, const uint32_t (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+
 struct PrefixMaps {
     CUtensorMap q, k[2], v[2];    // prefix, own
 };
@@ -273,9 +334,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     const uint32_t s_full = empty + 8 * RING, p_full = s_full + 16, o_full = p_full + 16;
     uint32_t* tmem_word = reinterpret_cast<uint32_t*>(rest + Shape::BARS * 8);
     long long* scan = reinterpret_cast<long long*>(rest + Shape::BARS * 8 + 16);        // [64]
+    float2* stat = reinterpret_cast<float2*>(scan + 64);        // [128] m and l of a row in the second set
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    constexpr int COPY_WARP = SETS * 4, MMA_WARP = COPY_WARP + 1, WARPS = MMA_WARP + 1;
+    constexpr int COPY_WARP = SETS * 4, MMA_WARP = COPY_WARP + 1, WARPS = Shape::THREADS / 32;
     if (tid == 0) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
@@ -332,7 +394,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             if (e < entries) {
                 x = prefix_entry<DIM>(a, e, bits);
                 s = steps_of(a, x);
-                r = rows_of<DIM>(a, x);
+                r = rows_of(a, x);
             }
             const long long si = warp_scan(s, lane), ri = warp_scan(r, lane);
             __syncthreads();
@@ -363,8 +425,12 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         walk.at = *found_at;
     }
 
+    // 384 threads are launched with 168 registers each (64512).  The softmax warps hold a row of 128 logits: they take 208, for
+    // which the third warpgroup goes down to 88 (128 * 88 + 256 * 208 = 64512).
     bool timed_out = false;
-    if (warp == COPY_WARP) {
+    if (warp >= COPY_WARP) {
+        if constexpr (SETS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == COPY_WARP) {
         // ------------------------------------- copies -------------------------------------
         int n = 0, p = 0;                                       // ring slots and pieces taken up so far
         while (!timed_out && walk.next(a)) {
@@ -384,7 +450,12 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             p++;
             __syncwarp();
-            auto load = [&](int tile, bool values) -> bool {
+            // in the order of the products (see there): K0 V0 K1 V1 ..., or K0 K1 V0 K2 V1 ... where tiles alternate
+            const int tiles = walk.tiles();
+#pragma unroll 1
+            for (int i = 0; i < 2 * tiles; i++, n++) {
+                const bool values = pair ? i & 1 : i & 1 ? i + 1 == 2 * tiles : i > 0;
+                const int tile = pair ? i >> 1 : values ? (i & 1 ? tiles : i >> 1) - 1 : (i + 1) >> 1;
                 int page = 0, place = 0;
                 if (lane < boxes) {
                     const int slot = (walk.u0 + tile) * SLOTS + lane * box, stretch = slot / c.page;
@@ -397,7 +468,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     }
                 }
                 const int s = n % RING;
-                if (n >= RING && !mbar_wait(empty + 8 * s, n / RING - 1, timed_out)) return false;
+                if (n >= RING && !mbar_wait(empty + 8 * s, n / RING - 1, timed_out)) break;
                 if (lane == 0) mbar_expect_tx(full + 8 * s, TILE);
                 __syncwarp();
                 if (lane < boxes) {
@@ -406,18 +477,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     for (int h = 0; h < HALVES; h++)
                         copy_slots(ring + s * TILE + h * (SLOTS * 128) + lane * box * 128, map, place, h, walk.head, page, full + 8 * s);
                 }
-                n++;
                 __syncwarp();
-                return true;
-            };
-            // in the order of the products: see there
-            const int tiles = walk.tiles();
-            if (!load(0, false)) break;
-            if (!pair && tiles > 1 && !load(1, false)) break;
-            for (int j = 0; j < tiles; j++) {
-                if (!load(j, true)) break;
-                const int ahead = j + (pair ? 1 : 2);
-                if (ahead < tiles && !load(ahead, false)) break;
             }
         }
         // the CTA must not end with copies in flight
@@ -431,11 +491,11 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             mbar_wait_sleep(q_full, p - 1, late);
             timed_out |= late;
         }
-    } else if (warp == MMA_WARP) {
+        } else if (warp == MMA_WARP) {
         // ------------------------------------- products -------------------------------------
         // Step x of a piece: tile x / 2 for set x % 2, or tile x where tiles alternate.  First the logits of steps 0 and 1, then the
         // values of step x and the logits of step x + 2: those of one set run while the other's exponentials are formed.
-        int n = 0, p = 0, uses[2] = {0, 0};                     // ring slots, pieces, products with either set's weights
+        int n = 0, p = 0, uses0 = 0, uses1 = 0;                 // ring slots, pieces, products with either set's weights
         while (!timed_out && walk.next(a)) {
             const int tiles = walk.tiles();
             if (tiles == 0) continue;
@@ -479,7 +539,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     fence_async_smem();
                     __syncwarp();
                 }
-                if (!mbar_wait(p_full + 8 * b, uses[b]++, timed_out)) return false;
+                if (!mbar_wait(p_full + 8 * b, b ? uses1++ : uses0++, timed_out)) return false;
                 tc_fence_after();
                 if (lane == 0) {
                     const uint32_t d = tmem + Shape::O_COL + set * DIM;
@@ -493,18 +553,24 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 __syncwarp();
                 return true;
             };
-            bool ok = logits(0) && (steps < 2 || logits(1));
-            for (int x = 0; ok && x < steps; x++) ok = values(x) && (x + 2 >= steps || logits(x + 2));
+            bool ok = true;
+#pragma unroll 1
+            for (int x = -2; ok && x < steps; x++) {
+                if (x >= 0) ok = values(x);
+                if (ok && x + 2 < steps) ok = logits(x + 2);
+            }
             if (!ok) break;
             n += 2 * tiles;
         }
+        }
     } else {
         // ------------------------------------- softmax -------------------------------------
+        if constexpr (SETS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int set = warp >> 2, row = 32 * (warp & 3) + lane;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const uint32_t o_at = tmem + lanes + Shape::O_COL + set * DIM;
         const int tok = row / a.group;
-        int s_uses[2] = {0, 0}, o_uses = 0;                     // logits taken from either place, products into O
+        int s_uses0 = 0, s_uses1 = 0, o_uses = 0;               // logits taken from either place, products into O
         while (!timed_out && walk.next(a)) {
             const bool pair = walk.pair(a);
             const int tiles = walk.tiles(), token = (walk.block * (pair ? 2 : 1) + (pair ? set : 0)) * a.block_tokens + tok;
@@ -517,11 +583,14 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             for (int x = SETS == 2 ? set : 0; x < steps; x += SETS) {
                 const int j = pair ? x >> 1 : x, b = x & 1;
                 const uint32_t s_at = tmem + lanes + b * 128;
-                if (!mbar_wait_warp(s_full + 8 * b, s_uses[b]++, timed_out)) break;
+                if (!mbar_wait_warp(s_full + 8 * b, b ? s_uses1++ : s_uses0++, timed_out)) break;
                 tc_fence_after();
                 uint32_t v[SLOTS / 32][32];
 #pragma unroll
-                for (int i = 0; i < SLOTS / 32; i++) tc_load32(s_at + 32 * i, v[i]);
+                for (int i = 0; i < SLOTS / 32; i++) tmem_load32(s_at + 32 * i, v[i]);
+                tmem_wait_load();
+#pragma unroll
+                for (int i = 0; i < SLOTS / 32; i++) tmem_loaded(v[i]);
                 const int left = limit - (walk.u0 + j) * SLOTS;  // slots of this tile that the row sees
                 if (__any_sync(0xffffffffu, left < SLOTS)) {
 #pragma unroll
@@ -530,8 +599,11 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 }
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < SLOTS; i++) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i / 32][i % 32]));
-                const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                for (int i = 0; i < SLOTS; i += 2) {
+                    float& t = top[(i >> 1) & 3];
+                    t = max3(t, __uint_as_float(v[i / 32][i % 32]), __uint_as_float(v[i / 32][i % 32 + 1]));
+                }
+                const float tile_top = max3(max3(top[0], top[1], top[2]), top[3], top[3]);
                 const bool rise = (tile_top - m) * a.scale_log2 > kLazyRise;     // (not for -inf after -inf)
                 float factor = 1.0f;
                 if (rise) {
@@ -552,22 +624,32 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     }
                 }
                 first = false;
-                const float base = m == -INFINITY ? 0.0f : kWeightBias<T> - m * a.scale_log2;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                // (a NaN among the logits makes the row NaN)
+                const float base = tile_top != tile_top ? tile_top : m == -INFINITY ? 0.0f : kWeightBias<T> - m * a.scale_log2;
+                const uint64_t scale2 = both(a.scale_log2, a.scale_log2), base2 = both(base, base);
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int i = 0; i < SLOTS / 32; i++) {
                     uint32_t w[16];
 #pragma unroll
                     for (int k = 0; k < 16; k++) {
-                        const float p0 = exp2_fast(fmaf(__uint_as_float(v[i][2 * k]), a.scale_log2, base));
-                        const float p1 = exp2_fast(fmaf(__uint_as_float(v[i][2 * k + 1]), a.scale_log2, base));
-                        sum[2 * (k & 1)] += p0;
-                        sum[2 * (k & 1) + 1] += p1;
+                        const uint64_t e = fma2(both(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), scale2, base2);
+                        float p0, p1;
+                        if (k % 4 == 3) {
+                            exp2_pair(e, p0, p1);
+                        } else {
+                            apart(e, p0, p1);
+                            p0 = exp2_fast(p0);
+                            p1 = exp2_fast(p1);
+                        }
+                        sum[k & 1] = add2(sum[k & 1], both(p0, p1));
                         w[k] = Pair<T>::pack(p0, p1);
                     }
                     tmem_store16(s_at + 16 * i, w);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                float s0, s1;
+                apart(add2(sum[0], sum[1]), s0, s1);
+                l += s0 + s1;
                 tmem_wait_store();
                 tc_fence_before();
                 __syncwarp();
@@ -576,24 +658,56 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             if (timed_out) break;
             // this piece's O, l and m
-            const long long store = walk.store(a) + (SETS == 2 ? (pair ? (long long)set * a.block_tokens : (long long)set * walk.e.tokens) : 0) * a.group + row;
-            if (!first) {
-                if (!mbar_wait_warp(o_full + 8 * set, o_uses - 1, timed_out)) break;
-                tc_fence_after();
+            if (!first && !mbar_wait_warp(o_full + 8 * set, o_uses - 1, timed_out)) break;
+            tc_fence_after();
+            const long long store = walk.store(a) + (pair && SETS == 2 ? set * a.block_tokens * a.group : 0) + row;
+            if (SETS == 2 && !pair) {
+                // both sets have a part of the same rows, in the same lanes: each puts half of the channels together
+                if (set == 1) stat[row] = make_float2(m, l);
+                named_sync(1, 256);
+                float f0 = 0.0f, f1 = 0.0f;
+                if (set == 0) {
+                    const float2 other = stat[row];
+                    const float most = fmaxf(m, other.x);
+                    f0 = m == -INFINITY ? 0.0f : exp2_fast((m - most) * a.scale_log2);
+                    f1 = other.x == -INFINITY ? 0.0f : exp2_fast((other.x - most) * a.scale_log2);
+                    l = (m == -INFINITY ? 0.0f : f0 * l) + (other.x == -INFINITY ? 0.0f : f1 * other.y);
+                    m = most;
+                    stat[row] = make_float2(f0, f1);
+                }
+                named_sync(1, 256);
+                if (set == 1) {
+                    f0 = stat[row].x;
+                    f1 = stat[row].y;
+                }
+                if (tiles > 0) {
+#pragma unroll 1
+                    for (int i = set * (DIM / 2); i < (set + 1) * (DIM / 2); i += 32) {
+                        uint32_t o[32], u[32];
+                        tmem_load32(tmem + lanes + Shape::O_COL + i, o);
+                        if (steps > 1) tmem_load32(tmem + lanes + Shape::O_COL + DIM + i, u);
+                        tmem_wait_load();
+                        tmem_loaded(o);
+                        if (steps > 1) {
+                            tmem_loaded(u);
+#pragma unroll
+                            for (int k = 0; k < 32; k++) o[k] = __float_as_uint(f0 * __uint_as_float(o[k]) + f1 * __uint_as_float(u[k]));
+                        }
+                        if (there) store32(a.partial + store * DIM + i, o);
+                    }
+                }
+                tc_fence_before();
+                named_sync(1, 256);                             // before either set's O is begun again
+            } else if (!first) {
 #pragma unroll 1
                 for (int i = 0; i < DIM; i += 32) {
                     uint32_t o[32];
                     tc_load32(o_at + i, o);
-                    if (there) {
-                        float4* to = reinterpret_cast<float4*>(a.partial + store * DIM + i);
-#pragma unroll
-                        for (int k = 0; k < 8; k++)
-                            to[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
-                    }
+                    if (there) store32(a.partial + store * DIM + i, o);
                 }
                 tc_fence_before();
             }
-            if (there) a.stats[store] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
+            if (there && (pair || set == 0)) a.stats[store] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
         }
     }
     tc_fence_before();
@@ -609,17 +723,18 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
 
 constexpr int kPrefixJoinThreads = 128;
 
-// One warp per (token, query head).
-template <typename T, int DIM>
+// WARPS warps per (token, query head), each taking every WARPS-th piece: four where rows are few and their pieces many.
+template <typename T, int DIM, int WARPS>
 __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid_constant__ PrefixArgs a) {
     constexpr int PER = DIM / 32;                               // channels per lane
-    const int lane = threadIdx.x & 31;
+    constexpr int AHEAD = 4;                                    // pieces whose O is on its way
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % WARPS;
     wait_for_prior_kernel();
     let_next_kernel_start();
-    const long long w = ((long long)blockIdx.x * kPrefixJoinThreads + threadIdx.x) >> 5;
+    const long long w = ((long long)blockIdx.x * kPrefixJoinThreads + threadIdx.x) / (32 * WARPS);
     const long long token = w / a.q_heads;
     const int qh = (int)(w - token * a.q_heads);
-    if (token >= a.rows || token < a.row_offsets[0] || token >= a.row_offsets[a.seqs]) return;
+    if (token >= a.rows || token < a.row_offsets[0] || token >= a.row_offsets[a.seqs]) return;     // (whole blocks where WARPS = 4)
     const PrefixHead head = *a.head;
     if (head.total < 0) return;
     const int seq = sequence_of(a.row_offsets, a.seqs, token, lane);
@@ -627,53 +742,75 @@ __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid
     if (a.seq_offsets != nullptr)
         of[0] = seq < a.seq_offsets[0] || seq >= a.seq_offsets[a.prefix.seqs] ? -1 : sequence_of(a.seq_offsets, a.prefix.seqs, seq, lane);
     const int kv = qh / a.group, g = qh - kv * a.group;
-    float top = -INFINITY, total = 0.0f, acc[PER];
-#pragma unroll
-    for (int i = 0; i < PER; i++) acc[i] = 0.0f;
+    // stored row of the first piece of either entry, and the number of pieces
+    long long at[2] = {0, 0};
+    int parts[2] = {0, 0};
     for (int which = 0; which < 2; which++) {
         if (of[which] < 0 || head.share == 0) continue;
         const PrefixEntry e = a.entries[of[which]];
-        if (e.units == 0 || e.tokens == 0) continue;
-        if (token < e.first || token >= e.first + e.tokens) continue;      // (offsets that go up and down)
-        const int in = (int)(token - e.first), copies = stored<DIM>(a, e);
-        const int per = alternates<DIM>(a, e) ? a.block_tokens : 2 * a.block_tokens;
-        const int block = in / per;
+        if (e.units == 0 || token < e.first || token >= e.first + e.tokens) continue;      // (offsets that go up and down)
+        const int in = (int)(token - e.first), block = in / (alternates<DIM>(a, e) ? a.block_tokens : 2 * a.block_tokens);
         const long long s0 = e.step0 + ((long long)kv * e.blocks + block) * e.units;
         const long long c0 = s0 / head.share, c1 = (s0 + e.units - 1) / head.share;
-        const long long at = e.row0 + (long long)kv * e.tokens * a.group * copies + (long long)in * a.group + g;
-        const int parts = (int)(c1 - c0 + 1) * copies;
-        for (int i0 = 0; i0 < parts; i0 += 32) {
-            // a lane looks after one piece's m and l
-            const int i = i0 + lane;
-            long long row = 0;
-            float2 s = make_float2(-INFINITY, 0.0f);
-            if (i < parts) {
-                row = (c0 + i / copies) * PrefixShape<DIM>::STORE + at + (long long)(i % copies) * e.tokens * a.group;
-                s = a.stats[row];
+        at[which] = c0 * PrefixShape<DIM>::STORE + e.row0 + ((long long)kv * e.tokens + in) * a.group + g;
+        parts[which] = (int)(c1 - c0) + 1;
+    }
+    auto row_of = [&](int i) { return i < parts[0] ? at[0] + (long long)i * PrefixShape<DIM>::STORE : at[1] + (long long)(i - parts[0]) * PrefixShape<DIM>::STORE; };
+    const int n = parts[0] + parts[1];
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, a.stats[row_of(i)].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float total = 0.0f, acc[PER];
+#pragma unroll
+    for (int i = 0; i < PER; i++) acc[i] = 0.0f;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        // a lane looks after one piece's m and l
+        float2 s = make_float2(-INFINITY, 0.0f);
+        if (i0 + lane < n) s = a.stats[row_of(i0 + lane)];
+        const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - top);
+        total += weight * s.y;
+        const int m = min(32, n - i0);
+        for (int k0 = warp; k0 < m; k0 += WARPS * AHEAD) {
+            float o[AHEAD][PER], f[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) {
+                const int k = k0 + u * WARPS;
+                f[u] = k < m ? __shfl_sync(0xffffffffu, weight, k) : 0.0f;
+                const float* from = a.partial + row_of(i0 + k) * DIM + lane * PER;
+                if (f[u] == 0.0f) {                             // (a piece without tiles stored no O)
+#pragma unroll
+                    for (int c = 0; c < PER; c++) o[u][c] = 0.0f;
+                } else if constexpr (PER == 2) {
+                    const float2 x = *reinterpret_cast<const float2*>(from);
+                    o[u][0] = x.x; o[u][1] = x.y;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < PER; c += 4) {
+                        const float4 x = *reinterpret_cast<const float4*>(from + c);
+                        o[u][c] = x.x; o[u][c + 1] = x.y; o[u][c + 2] = x.z; o[u][c + 3] = x.w;
+                    }
+                }
             }
-            float most = s.x;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            const float now = fmaxf(top, most), keep = top == -INFINITY ? 0.0f : exp2f(top - now);
-            const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - now);
-            top = now;
-            total *= keep;
+            for (int u = 0; u < AHEAD; u++)
 #pragma unroll
-            for (int k = 0; k < PER; k++) acc[k] *= keep;
-            float sum = weight * s.y;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            total += sum;
-            const int n = min(32, parts - i0);
-            for (int k = 0; k < n; k++) {
-                const float f = __shfl_sync(0xffffffffu, weight, k);
-                const long long r = __shfl_sync(0xffffffffu, row, k);
-                if (f == 0.0f) continue;                        // (a piece without tiles stored no O)
-                const float* from = a.partial + r * DIM + lane * PER;
-#pragma unroll
-                for (int c = 0; c < PER; c++) acc[c] += f * from[c];
-            }
+                for (int c = 0; c < PER; c++) acc[c] += f[u] * o[u][c];
         }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if constexpr (WARPS > 1) {
+        __shared__ float parked[WARPS - 1][DIM];
+        if (warp > 0)
+#pragma unroll
+            for (int c = 0; c < PER; c++) parked[warp - 1][c * 32 + lane] = acc[c];
+        __syncthreads();
+        if (warp > 0) return;
+#pragma unroll
+        for (int k = 0; k < WARPS - 1; k++)
+#pragma unroll
+            for (int c = 0; c < PER; c++) acc[c] += parked[k][c * 32 + lane];
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (token * a.q_heads + qh) * DIM + lane * PER);
