@@ -193,28 +193,46 @@ __host__ __device__ constexpr uint32_t attend_idesc(int n, bool b_by_n) {
     const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
     return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)b_by_n << 16) | ((uint32_t)(n / 8) << 17) | (8u << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// (The descriptors of a warp's products differ in their low words alone.  The instruction wants them in uniform registers: moving
+// there what the compiler takes for a value of one thread costs more than the product, see one_value.)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 da, {%1, %2};\n\t"
+        "mov.b64 db, {%3, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 // A in tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// one lane of the warp
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+// a value that is the same in every lane, told to the compiler
+__device__ __forceinline__ uint32_t one_value(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 // Operand whose row axis (channels) is contiguous, 128-byte swizzle: groups of eight slots 1024 bytes apart, 64-channel
 // parts `part` bytes apart.
 __device__ __forceinline__ uint64_t operand_by_n(uint32_t addr, uint32_t part) {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(part >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
+constexpr uint32_t kOperandHigh = (1024 >> 4) | (1u << 14) | (2u << 29);        // the high word of both kinds
 __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -512,16 +530,17 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 const int i = n + key_slot(j), s = i % RING;
                 if (!mbar_wait(full + 8 * s, i / RING, timed_out)) return false;
                 tc_fence_after();
-                if (lane == 0) {
+                const uint32_t a_lo = one_value((uint32_t)tc_operand(qmem + set * Shape::QBLOCK)), b_lo = one_value((uint32_t)tc_operand(ring + s * TILE));
+                const uint32_t d = one_value(tmem + b * 128), last = one_value(x + 1 == steps), frees = one_value(!pair || b == 1);
+                const uint32_t done = one_value(s_full + 8 * b), free_at = one_value(empty + 8 * s);
+                if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < DIM / 16; k++) {
-                        const uint32_t in = (k & 3) * 32;
-                        mma_ss(tmem + b * 128, tc_operand(qmem + set * Shape::QBLOCK + (k >> 2) * (128 * 128) + in),
-                               tc_operand(ring + s * TILE + (k >> 2) * (SLOTS * 128) + in), attend_idesc<T>(SLOTS, false), k > 0);
-                    }
-                    tc_commit(s_full + 8 * b);
-                    if (!pair || b == 1) tc_commit(empty + 8 * s);
-                    if (x + 1 == steps) tc_commit(q_empty);
+                    for (int k = 0; k < DIM / 16; k++)
+                        mma_ss(d, a_lo + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, kOperandHigh, b_lo + (k >> 2) * (SLOTS * 128 / 16) + (k & 3) * 2, kOperandHigh,
+                               attend_idesc<T>(SLOTS, false), k > 0);
+                    tc_commit(done);
+                    if (frees) tc_commit(free_at);
+                    if (last) tc_commit(q_empty);
                 }
                 __syncwarp();
                 return true;
@@ -541,14 +560,14 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 }
                 if (!mbar_wait(p_full + 8 * b, b ? uses1++ : uses0++, timed_out)) return false;
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t d = tmem + Shape::O_COL + set * DIM;
+                const uint32_t d = one_value(tmem + Shape::O_COL + set * DIM), p_at = one_value(tmem + b * 128), more = one_value(x >= SETS);
+                const uint32_t v_lo = one_value((uint32_t)operand_by_n(ring + s * TILE, SLOTS * 128)), frees = one_value(!pair || b == 1);
+                const uint32_t done = one_value(o_full + 8 * set), free_at = one_value(empty + 8 * s);
+                if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < SLOTS / 16; k++)
-                        mma_ts(d, tmem + b * 128 + k * 8, operand_by_n(ring + s * TILE + k * 2048, SLOTS * 128), attend_idesc<T>(DIM, true),
-                               x >= SETS || k > 0);
-                    tc_commit(o_full + 8 * set);
-                    if (!pair || b == 1) tc_commit(empty + 8 * s);
+                    for (int k = 0; k < SLOTS / 16; k++) mma_ts(d, p_at + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), k > 0 ? 1 : more);
+                    tc_commit(done);
+                    if (frees) tc_commit(free_at);
                 }
                 __syncwarp();
                 return true;
