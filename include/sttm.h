@@ -430,7 +430,7 @@ sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const
 typedef struct sttm_prefix_params {
     const void* q;                /* [rows][q_heads][dim], 16-byte aligned                         */
     long long q_row, q_head;      /* strides in elements, multiples of 8                           */
-    long long rows;               /* rows behind q, below 2^31                                     */
+    long long rows;               /* rows behind q; rows * q_heads below 2^31                      */
     int q_heads;                  /* a multiple of the cache's heads, at most 64 per KV head       */
     int seqs;
     const int64_t* row_offsets;   /* [seqs + 1], not decreasing                                    */

@@ -42,7 +42,7 @@ struct PrefixArgs {
     struct PrefixHead* head;      // workspace
     struct PrefixEntry* entries;
     float2* stats;                // per stored row: m (times c, in powers of two) and l
-    float* partial;               // per stored row: O
+    float* partial;               // O of the stored rows: per block of rows [dim / 4][rows][4]
 };
 
 struct PrefixHead {
@@ -62,9 +62,9 @@ struct PrefixShape {
     static constexpr int HALVES = DIM / 64;                     // 64-channel parts of 128 bytes per row
     static constexpr int TILE = SLOTS * DIM * 2, QBLOCK = 128 * DIM * 2;
     static constexpr int RING = DIM == 64 ? 10 : 5;
-    static constexpr int THREADS = SETS == 2 ? 384 : 192;       // softmax warps, the two others (and two idle ones: see the register split)
+    static constexpr int THREADS = SETS * 128 + 128;            // softmax warps, one that issues the products, three that copy
     static constexpr uint32_t O_COL = 256;                      // S at columns 0 and 128, O from here on
-    static constexpr int BARS = 2 + 2 * RING + 6;
+    static constexpr int BARS = 2 + 2 * RING + 8;
     static constexpr size_t SMEM = (size_t)SETS * QBLOCK + (size_t)RING * TILE + BARS * 8 + 16 + 64 * 8 + 128 * 8 + 1024;
     static constexpr int STORE = SETS * 128;                    // stored rows of a piece at most
 };
@@ -77,6 +77,7 @@ constexpr float kWeightBias<__half> = 4.0f;
 
 constexpr float kLazyRise = 8.0f;                               // powers of two
 constexpr int kPieceSteps = 3;
+constexpr int kCopyWarps = 3;
 
 // ---- entries ----
 
@@ -135,6 +136,11 @@ __device__ __forceinline__ bool alternates(const PrefixArgs& a, const PrefixEntr
 __device__ __forceinline__ long long steps_of(const PrefixArgs& a, const PrefixEntry& e) { return (long long)a.prefix.heads * e.blocks * e.units; }
 __device__ __forceinline__ long long rows_of(const PrefixArgs& a, const PrefixEntry& e) { return e.units ? (long long)a.q_heads * e.tokens : 0; }
 
+// (a division in 64 bits takes some hundred instructions)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 __device__ __forceinline__ long long warp_scan(long long v, int lane) {
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
@@ -161,7 +167,7 @@ struct PieceWalk {
             e.row0 = r;
         }
         const long long in = step - e.step0;
-        item = (int)(in / e.units);
+        item = (int)quotient(in, e.units);
         const int from = (int)(in - (long long)item * e.units), to = (int)min((long long)e.units, from + (end - step));
         step += to - from;
         u0 = max(0, from - kPieceSteps);
@@ -179,9 +185,12 @@ struct PieceWalk {
     __device__ __forceinline__ bool is_own(const PrefixArgs& a) const { return at >= a.prefix.seqs; }
     __device__ __forceinline__ int tiles() const { return u1 - u0; }
     __device__ __forceinline__ bool pair(const PrefixArgs& a) const { return !alternates<DIM>(a, e); }
-    // first stored row
-    __device__ __forceinline__ long long store(const PrefixArgs& a) const {
-        return (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + ((long long)head * e.tokens + (long long)block * (pair(a) ? 2 : 1) * a.block_tokens) * a.group;
+    // rows (token, query head) of a set's block, and the first of them in memory
+    __device__ __forceinline__ int set_rows(const PrefixArgs& a, int set) const {
+        return min(a.block_tokens, max(0, e.tokens - (block * (pair(a) ? 2 : 1) + set) * a.block_tokens)) * a.group;
+    }
+    __device__ __forceinline__ long long store(const PrefixArgs& a, int set) const {
+        return (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + ((long long)head * e.tokens + (long long)(block * (pair(a) ? 2 : 1) + set) * a.block_tokens) * a.group;
     }
 };
 
@@ -330,9 +339,25 @@ __device__ __forceinline__ void copy_slots(uint32_t dst, const CUtensorMap* map,
         : "memory");
 }
 
-__device__ __forceinline__ void store32(float* to, const uint32_t (&v)[32]) {
+// 32 channels of a row: four at a time, those of one set's rows beside each other, so that a warp writes whole stretches
+__device__ __forceinline__ void store32(float4* to, int rows, const uint32_t (&v)[32]) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    for (int i = 0; i < 8; i++)
+        to[i * rows] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+}
+
+// Bounded wait of a warp for the `use`-th completion of an mbarrier of this CTA (see mbar_wait).  It polls; its acquire reaches no further than
+// the CTA: the one over a cluster costs some 200 cycles more, several times per tile.
+__device__ __forceinline__ bool mbar_wait_near(uint32_t bar, int use, bool& timed_out) {
+    const uint32_t parity = (uint32_t)(use & 1);
+    bool ok = !timed_out;
+    if (ok && !mbar_try(bar, parity)) {
+        const unsigned long long t0 = global_timer_ns();
+        while (ok && !mbar_try(bar, parity)) ok = global_timer_ns() - t0 <= kWaitLimitNs;
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    timed_out = !ok;
+    return ok;
 }
 
 struct PrefixMaps {
@@ -349,7 +374,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     const uint32_t qmem = smem_u32(smem), ring = qmem + SETS * Shape::QBLOCK;
     unsigned char* rest = smem + SETS * Shape::QBLOCK + RING * TILE;
     const uint32_t q_full = smem_u32(rest), q_empty = q_full + 8, full = q_full + 16, empty = full + 8 * RING;
-    const uint32_t s_full = empty + 8 * RING, p_full = s_full + 16, o_full = p_full + 16;
+    const uint32_t s_full = empty + 8 * RING, p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16;
     uint32_t* tmem_word = reinterpret_cast<uint32_t*>(rest + Shape::BARS * 8);
     long long* scan = reinterpret_cast<long long*>(rest + Shape::BARS * 8 + 16);        // [64]
     float2* stat = reinterpret_cast<float2*>(scan + 64);        // [128] m and l of a row in the second set
@@ -360,11 +385,12 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         for (int s = 0; s < RING; s++) {
-            mbar_init(full + 8 * s, 1);
+            mbar_init(full + 8 * s, kCopyWarps);
             mbar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; b++) {
             mbar_init(s_full + 8 * b, 1);
+            mbar_init(p_half + 8 * b, 4);
             mbar_init(p_full + 8 * b, 4);
             mbar_init(o_full + 8 * b, 1);
         }
@@ -448,55 +474,89 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     bool timed_out = false;
     if (warp >= COPY_WARP) {
         if constexpr (SETS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp == COPY_WARP) {
+        if (warp != MMA_WARP) {
         // ------------------------------------- copies -------------------------------------
+        // Issuing a tensor copy keeps a warp busy for some 80 cycles whatever its size, and small pages make many of them: the
+        // boxes of a tile (a box of slots, 64 channels) are shared between three warps, one box to a lane.
+        const int part = warp == COPY_WARP ? 0 : warp - MMA_WARP;
         int n = 0, p = 0;                                       // ring slots and pieces taken up so far
         while (!timed_out && walk.next(a)) {
-            if (walk.tiles() == 0) continue;
-            const bool pair = walk.pair(a);
-            const int own = walk.is_own(a), sets = pair ? 2 : 1;
-            const CacheView& c = own ? a.own : a.prefix;
-            const int box = a.page_box[own], boxes = SLOTS / box, row = own ? walk.at - a.prefix.seqs : walk.at;
-            if (p > 0 && !mbar_wait(q_empty, p - 1, timed_out)) break;
-            if (lane == 0) {
-                const int bytes = a.block_tokens * a.group * 128;
-                mbar_expect_tx(q_full, sets * HALVES * bytes);
-                for (int t = 0; t < sets; t++)
-                    for (int h = 0; h < HALVES; h++)
-                        copy_queries(qmem + t * Shape::QBLOCK + h * (128 * 128), &maps.q, walk.head * a.group, h,
-                                     (int)(walk.e.first + (long long)(walk.block * sets + t) * a.block_tokens), q_full);
-            }
-            p++;
-            __syncwarp();
-            // in the order of the products (see there): K0 V0 K1 V1 ..., or K0 K1 V0 K2 V1 ... where tiles alternate
             const int tiles = walk.tiles();
-#pragma unroll 1
-            for (int i = 0; i < 2 * tiles; i++, n++) {
-                const bool values = pair ? i & 1 : i & 1 ? i + 1 == 2 * tiles : i > 0;
-                const int tile = pair ? i >> 1 : values ? (i & 1 ? tiles : i >> 1) - 1 : (i + 1) >> 1;
-                int page = 0, place = 0;
-                if (lane < boxes) {
-                    const int slot = (walk.u0 + tile) * SLOTS + lane * box, stretch = slot / c.page;
-                    place = slot - stretch * c.page;
-                    page = (int)c.pages;                        // beyond the pool: zeros
-                    if (slot < walk.e.len) {
-                        const int pg = c.table[row * c.table_stride + stretch];
-                        if (pg >= 0 && pg < c.pages) page = pg;
-                        else raise_status(a.status, kStatusArg);
-                    }
+            if (tiles == 0) continue;
+            const bool pair = walk.pair(a);
+            const int own = walk.is_own(a);
+            const CacheView& c = own ? a.own : a.prefix;
+            const int box = a.page_box[own], page_slots = c.page, pages = (int)c.pages;
+            const int32_t* table = c.table + (own ? walk.at - a.prefix.seqs : walk.at) * c.table_stride;
+            const int at = lane * kCopyWarps + part, in_tile = at / HALVES * box, half = at % HALVES;
+            const bool copies = in_tile < SLOTS;
+            // Page (`pages`, beyond the pool: zeros) and place in it of this lane's box, by the tile's number modulo four; looked up two
+            // tiles ahead.
+            int page[4], place[4];
+            const int slot0 = walk.u0 * SLOTS + in_tile, by_pages = SLOTS / page_slots, by_slots = SLOTS % page_slots;
+            int left = walk.e.len - slot0, stretch = slot0 / page_slots, spot = slot0 - stretch * page_slots;     // of the tile looked up next
+            auto look_up = [&](int& pg, int& pl) {
+                pg = pages;
+                pl = spot;
+                if (copies && left > 0) {
+                    pg = table[stretch];
+                    if (pg == pages) pg = -1;
                 }
+                left -= SLOTS;
+                stretch += by_pages;
+                spot += by_slots;
+                if (spot >= page_slots) {
+                    spot -= page_slots;
+                    stretch++;
+                }
+            };
+            const uint32_t to = ring + half * (SLOTS * 128) + in_tile * 128;
+            const uint32_t bytes = ((SLOTS / box * HALVES + kCopyWarps - 1 - part) / kCopyWarps) * box * 128;      // this warp's of a tile
+            auto copy = [&](const CUtensorMap* map, int pg, int pl) -> bool {
                 const int s = n % RING;
-                if (n >= RING && !mbar_wait(empty + 8 * s, n / RING - 1, timed_out)) break;
-                if (lane == 0) mbar_expect_tx(full + 8 * s, TILE);
+                if (n >= RING && !mbar_wait_near(empty + 8 * s, n / RING - 1, timed_out)) return false;
+                if (lane == 0) mbar_expect_tx(full + 8 * s, bytes);
                 __syncwarp();
-                if (lane < boxes) {
-                    const CUtensorMap* map = values ? &maps.v[own] : &maps.k[own];
-#pragma unroll
-                    for (int h = 0; h < HALVES; h++)
-                        copy_slots(ring + s * TILE + h * (SLOTS * 128) + lane * box * 128, map, place, h, walk.head, page, full + 8 * s);
+                if (copies) {
+                    if (pg < 0 || pg > pages) {
+                        raise_status(a.status, kStatusArg);
+                        pg = pages;
+                    }
+                    copy_slots(to + s * TILE, map, pl, half, walk.head, pg, full + 8 * s);
+                }
+                n++;
+                return true;
+            };
+            look_up(page[0], place[0]);
+            look_up(page[1], place[1]);
+            if (part == 0) {
+                if (p > 0 && !mbar_wait_near(q_empty, p - 1, timed_out)) break;
+                if (lane == 0) {
+                    const int sets = pair ? 2 : 1, q_bytes = a.block_tokens * a.group * 128;
+                    mbar_expect_tx(q_full, sets * HALVES * q_bytes);
+                    for (int t = 0; t < sets; t++)
+                        for (int h = 0; h < HALVES; h++)
+                            copy_queries(qmem + t * Shape::QBLOCK + h * (128 * 128), &maps.q, walk.head * a.group, h,
+                                         (int)(walk.e.first + (long long)(walk.block * sets + t) * a.block_tokens), q_full);
                 }
                 __syncwarp();
+                p++;
             }
+            // In the order in which the products want them, K0 V0 K1 V1 ..., or K0 K1 V0 K2 V1 ... where tiles alternate: keys of tile j,
+            // values of the tile one or two before.
+            const int behind = pair ? 1 : 2;
+            bool ok = true;
+            for (int j0 = 0; ok && j0 < tiles + behind; j0 += 4) {
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    const int j = j0 + u;
+                    if (ok && j >= behind && j < tiles + behind)
+                        ok = pair ? copy(&maps.v[own], page[(u + 3) & 3], place[(u + 3) & 3]) : copy(&maps.v[own], page[(u + 2) & 3], place[(u + 2) & 3]);
+                    if (ok && j < tiles) ok = copy(&maps.k[own], page[u], place[u]);
+                    look_up(page[(u + 2) & 3], place[(u + 2) & 3]);
+                }
+            }
+            if (!ok) break;
         }
         // the CTA must not end with copies in flight
         for (int i = max(0, n - RING); i < n; i++) {
@@ -509,77 +569,130 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             mbar_wait_sleep(q_full, p - 1, late);
             timed_out |= late;
         }
-        } else if (warp == MMA_WARP) {
+        } else {
         // ------------------------------------- products -------------------------------------
         // Step x of a piece: tile x / 2 for set x % 2, or tile x where tiles alternate.  First the logits of steps 0 and 1, then the
-        // values of step x and the logits of step x + 2: those of one set run while the other's exponentials are formed.
-        int n = 0, p = 0, uses0 = 0, uses1 = 0;                 // ring slots, pieces, products with either set's weights
+        // values of step x and the logits of step x + 2: those of one set run while the other's exponentials are formed.  Between two
+        // products this warp's own instructions, one dependent on the other, are time in which the tensor cores idle: ring slots are
+        // counted up as they are taken (in the order in which the copies fill them), addresses are ready before the waits.
+        int p = 0;                                              // pieces
+        uint32_t slot = 0, turn = 0, weights_turn[2] = {0, 0};  // ring slot taken next; parities of its, and of the weights', next wait
+        const uint32_t q_lo = one_value((uint32_t)tc_operand(qmem)), ring_lo = one_value((uint32_t)tc_operand(ring));
+        const uint32_t ring_by_n = one_value((uint32_t)operand_by_n(ring, SLOTS * 128)), tm = one_value(tmem), bars = one_value(smem_u32(rest));
+        const uint32_t o_full_u = bars + (o_full - q_full), s_full_u = bars + (s_full - q_full), empty_u = bars + (empty - q_full);
+        auto take = [&](uint32_t& taken) -> bool {
+            taken = slot;
+            const bool ok = mbar_wait_near(full + 8 * slot, turn, timed_out);
+            if (++slot == RING) {
+                slot = 0;
+                turn ^= 1;
+            }
+            return ok;
+        };
         while (!timed_out && walk.next(a)) {
             const int tiles = walk.tiles();
             if (tiles == 0) continue;
             const bool pair = walk.pair(a);
-            const int steps = pair ? 2 * tiles : tiles;
-            if (!mbar_wait(q_full, p, timed_out)) break;
-            p++;
-            tc_fence_after();
-            // ring slot (counted from the piece's first) of a tile's keys and values
-            auto key_slot = [&](int j) { return pair ? 2 * j : j < 2 ? j : 2 * j - 1; };
-            auto value_slot = [&](int j) { return pair ? 2 * j + 1 : j + 1 < tiles ? 2 * j + 2 : 2 * j + 1; };
-            auto logits = [&](int x) -> bool {
-                const int j = pair ? x >> 1 : x, b = x & 1, set = pair ? b : 0;
-                const int i = n + key_slot(j), s = i % RING;
-                if (!mbar_wait(full + 8 * s, i / RING, timed_out)) return false;
-                tc_fence_after();
-                const uint32_t a_lo = one_value((uint32_t)tc_operand(qmem + set * Shape::QBLOCK)), b_lo = one_value((uint32_t)tc_operand(ring + s * TILE));
-                const uint32_t d = one_value(tmem + b * 128), last = one_value(x + 1 == steps), frees = one_value(!pair || b == 1);
-                const uint32_t done = one_value(s_full + 8 * b), free_at = one_value(empty + 8 * s);
+            // logits of set (place) b
+            auto logits = [&](auto place, int set, uint32_t k_slot, bool frees, bool last) {
+                constexpr int b = decltype(place)::value;
+                const uint32_t at = one_value(k_slot), a_lo = q_lo + (SETS == 2 && set ? Shape::QBLOCK / 16 : 0), b_lo = ring_lo + at * (TILE / 16);
                 if (elected()) {
 #pragma unroll
                     for (int k = 0; k < DIM / 16; k++)
-                        mma_ss(d, a_lo + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, kOperandHigh, b_lo + (k >> 2) * (SLOTS * 128 / 16) + (k & 3) * 2, kOperandHigh,
-                               attend_idesc<T>(SLOTS, false), k > 0);
-                    tc_commit(done);
-                    if (frees) tc_commit(free_at);
-                    if (last) tc_commit(q_empty);
+                        mma_ss(tm + b * 128, a_lo + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, kOperandHigh, b_lo + (k >> 2) * (SLOTS * 128 / 16) + (k & 3) * 2,
+                               kOperandHigh, attend_idesc<T>(SLOTS, false), k > 0);
+                    tc_commit(s_full_u + 8 * b);
+                    if (frees) tc_commit(empty_u + 8 * at);
+                    if (last) tc_commit(bars + 8);              // q_empty
                 }
                 __syncwarp();
-                return true;
             };
-            auto values = [&](int x) -> bool {
-                const int j = pair ? x >> 1 : x, b = x & 1, set = SETS == 2 ? b : 0;
-                const int i = n + value_slot(j), s = i % RING;
-                if (!mbar_wait(full + 8 * s, i / RING, timed_out)) return false;
-                const int there = walk.e.len - (walk.u0 + j) * SLOTS;
-                if (there < SLOTS && (!pair || b == 0)) {       // what lies behind the last slot may be anything: 0 times it must be 0
-                    for (int w = lane; w < (SLOTS - there) * 8 * HALVES; w += 32) {
-                        const int h = w / ((SLOTS - there) * 8), u = w - h * (SLOTS - there) * 8;
-                        *reinterpret_cast<uint4*>(smem + SETS * Shape::QBLOCK + s * TILE + h * (SLOTS * 128) + there * 128 + u * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async_smem();
-                    __syncwarp();
-                }
-                if (!mbar_wait(p_full + 8 * b, b ? uses1++ : uses0++, timed_out)) return false;
+            // weights of place b times the values
+            auto values = [&](auto place, uint32_t v_slot, bool more, bool frees) -> bool {
+                constexpr int b = decltype(place)::value, set = SETS == 2 ? b : 0;
+                const uint32_t at = one_value(v_slot), v_lo = ring_by_n + at * (TILE / 16), d = tm + Shape::O_COL + set * DIM;
+                if (!mbar_wait_near(p_half + 8 * b, weights_turn[b], timed_out)) return false;
                 tc_fence_after();
-                const uint32_t d = one_value(tmem + Shape::O_COL + set * DIM), p_at = one_value(tmem + b * 128), more = one_value(x >= SETS);
-                const uint32_t v_lo = one_value((uint32_t)operand_by_n(ring + s * TILE, SLOTS * 128)), frees = one_value(!pair || b == 1);
-                const uint32_t done = one_value(o_full + 8 * set), free_at = one_value(empty + 8 * s);
                 if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < SLOTS / 16; k++) mma_ts(d, p_at + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), k > 0 ? 1 : more);
-                    tc_commit(done);
-                    if (frees) tc_commit(free_at);
+                    for (int k = 0; k < SLOTS / 32; k++)
+                        mma_ts(d, tm + b * 128 + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), k > 0 ? 1 : more);
+                }
+                __syncwarp();
+                if (!mbar_wait_near(p_full + 8 * b, weights_turn[b], timed_out)) return false;
+                weights_turn[b] ^= 1;
+                tc_fence_after();
+                if (elected()) {
+#pragma unroll
+                    for (int k = SLOTS / 32; k < SLOTS / 16; k++)
+                        mma_ts(d, tm + b * 128 + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), 1);
+                    tc_commit(o_full_u + 8 * set);
+                    if (frees) tc_commit(empty_u + 8 * at);
                 }
                 __syncwarp();
                 return true;
             };
+            // What lies behind the last slot may be anything: 0 times it must be 0.
+            auto clear_tail = [&](int j, uint32_t v_slot) {
+                const int there = walk.e.len - (walk.u0 + j) * SLOTS;
+                if (j + 1 < tiles || there >= SLOTS) return;
+                for (int w = lane; w < (SLOTS - there) * 8 * HALVES; w += 32) {
+                    const int h = w / ((SLOTS - there) * 8), u = w - h * (SLOTS - there) * 8;
+                    *reinterpret_cast<uint4*>(smem + SETS * Shape::QBLOCK + v_slot * TILE + h * (SLOTS * 128) + there * 128 + u * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async_smem();
+                __syncwarp();
+            };
+            const std::integral_constant<int, 0> zero{};
+            const std::integral_constant<int, 1> one{};
+            uint32_t ks = 0, vs = 0;
+            if (!mbar_wait_near(q_full, p, timed_out) || !take(ks)) break;
+            p++;
             bool ok = true;
+            if (pair) {
+                logits(zero, 0, ks, false, false);
+                logits(one, 1, ks, true, tiles == 1);
 #pragma unroll 1
-            for (int x = -2; ok && x < steps; x++) {
-                if (x >= 0) ok = values(x);
-                if (ok && x + 2 < steps) ok = logits(x + 2);
+                for (int j = 0; j < tiles; j++) {
+                    const bool more = j + 1 < tiles;
+                    if (!(ok = take(vs))) break;
+                    clear_tail(j, vs);
+                    if (!(ok = values(zero, vs, j > 0, false))) break;
+                    if (more) {
+                        if (!(ok = take(ks))) break;
+                        logits(zero, 0, ks, false, false);
+                    }
+                    if (!(ok = values(one, vs, j > 0, true))) break;
+                    if (more) logits(one, 1, ks, true, j + 2 == tiles);
+                }
+            } else {
+                logits(zero, 0, ks, true, tiles == 1);
+                if (tiles > 1) {
+                    if (!take(ks)) break;
+                    logits(one, 0, ks, true, tiles == 2);
+                }
+#pragma unroll 1
+                for (int j = 0; j < tiles; j += 2) {
+                    if (!(ok = take(vs))) break;
+                    clear_tail(j, vs);
+                    if (!(ok = values(zero, vs, j > 0, true))) break;
+                    if (j + 2 < tiles) {
+                        if (!(ok = take(ks))) break;
+                        logits(zero, 0, ks, true, j + 3 == tiles);
+                    }
+                    if (j + 1 < tiles) {
+                        if (!(ok = take(vs))) break;
+                        clear_tail(j + 1, vs);
+                        if (!(ok = values(one, vs, SETS == 1 || j > 0, true))) break;
+                        if (j + 3 < tiles) {
+                            if (!(ok = take(ks))) break;
+                            logits(one, 0, ks, true, j + 4 == tiles);
+                        }
+                    }
+                }
             }
             if (!ok) break;
-            n += 2 * tiles;
         }
         }
     } else {
@@ -602,7 +715,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             for (int x = SETS == 2 ? set : 0; x < steps; x += SETS) {
                 const int j = pair ? x >> 1 : x, b = x & 1;
                 const uint32_t s_at = tmem + lanes + b * 128;
-                if (!mbar_wait_warp(s_full + 8 * b, b ? s_uses1++ : s_uses0++, timed_out)) break;
+                if (!mbar_wait_near(s_full + 8 * b, b ? s_uses1++ : s_uses0++, timed_out)) break;
                 tc_fence_after();
                 uint32_t v[SLOTS / 32][32];
 #pragma unroll
@@ -630,7 +743,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     m = tile_top;
                 }
                 if (!first && __any_sync(0xffffffffu, rise)) {
-                    if (!mbar_wait_warp(o_full + 8 * set, o_uses - 1, timed_out)) break;
+                    if (!mbar_wait_near(o_full + 8 * set, o_uses - 1, timed_out)) break;
                     tc_fence_after();
                     l *= factor;
 #pragma unroll 1
@@ -665,6 +778,12 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                         w[k] = Pair<T>::pack(p0, p1);
                     }
                     tmem_store16(s_at + 16 * i, w);
+                    if (i + 1 == SLOTS / 64) {                  // the product begins with the first half of the weights
+                        tmem_wait_store();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(p_half + 8 * b);
+                    }
                 }
                 float s0, s1;
                 apart(add2(sum[0], sum[1]), s0, s1);
@@ -677,9 +796,11 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             if (timed_out) break;
             // this piece's O, l and m
-            if (!first && !mbar_wait_warp(o_full + 8 * set, o_uses - 1, timed_out)) break;
+            if (!first && !mbar_wait_near(o_full + 8 * set, o_uses - 1, timed_out)) break;
             tc_fence_after();
-            const long long store = walk.store(a) + (pair && SETS == 2 ? set * a.block_tokens * a.group : 0) + row;
+            const int rows = walk.set_rows(a, pair ? set : 0);
+            const long long store = walk.store(a, pair ? set : 0);
+            float4* const to = reinterpret_cast<float4*>(a.partial + store * DIM) + row;
             if (SETS == 2 && !pair) {
                 // both sets have a part of the same rows, in the same lanes: each puts half of the channels together
                 if (set == 1) stat[row] = make_float2(m, l);
@@ -712,7 +833,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
 #pragma unroll
                             for (int k = 0; k < 32; k++) o[k] = __float_as_uint(f0 * __uint_as_float(o[k]) + f1 * __uint_as_float(u[k]));
                         }
-                        if (there) store32(a.partial + store * DIM + i, o);
+                        if (there) store32(to + (i / 4) * rows, rows, o);
                     }
                 }
                 tc_fence_before();
@@ -722,11 +843,11 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 for (int i = 0; i < DIM; i += 32) {
                     uint32_t o[32];
                     tc_load32(o_at + i, o);
-                    if (there) store32(a.partial + store * DIM + i, o);
+                    if (there) store32(to + (i / 4) * rows, rows, o);
                 }
                 tc_fence_before();
             }
-            if (there && (pair || set == 0)) a.stats[store] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
+            if (there && (pair || set == 0)) a.stats[store + row] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
         }
     }
     tc_fence_before();
@@ -740,102 +861,115 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
 
 // ---- pieces of a row to its output ----
 
-constexpr int kPrefixJoinThreads = 128;
+constexpr int kJoinRows = 8;                                    // rows (token, query head of one KV head) per block
+constexpr int kJoinParts = 320;                                 // pieces of a row at most: two entries' over all CTAs
 
-// WARPS warps per (token, query head), each taking every WARPS-th piece: four where rows are few and their pieces many.
-template <typename T, int DIM, int WARPS>
-__global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid_constant__ PrefixArgs a) {
-    constexpr int PER = DIM / 32;                               // channels per lane
-    constexpr int AHEAD = 4;                                    // pieces whose O is on its way
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % WARPS;
+template <int DIM>
+constexpr int kPrefixJoinThreads = kJoinRows * DIM / 4;
+
+// A block puts eight rows together; its threads take four channels of a row each, rows beside each other as the pieces store them.
+// First a warp per row finds the row's pieces and their weights.
+template <typename T, int DIM>
+__global__ void __launch_bounds__(kPrefixJoinThreads<DIM>) k_prefix_join(const __grid_constant__ PrefixArgs a) {
+    constexpr int WARPS = kPrefixJoinThreads<DIM> / 32, AHEAD = 8;
+    struct Row {
+        const float4* from[2];    // the row's first four channels in its first piece
+        int parts[2], rows[2];    // pieces; rows of the block that they lie in
+        float inv;
+    };
+    __shared__ Row found[kJoinRows];
+    __shared__ float weights[kJoinRows][kJoinParts];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     wait_for_prior_kernel();
     let_next_kernel_start();
-    const long long w = ((long long)blockIdx.x * kPrefixJoinThreads + threadIdx.x) / (32 * WARPS);
-    const long long token = w / a.q_heads;
-    const int qh = (int)(w - token * a.q_heads);
-    if (token >= a.rows || token < a.row_offsets[0] || token >= a.row_offsets[a.seqs]) return;     // (whole blocks where WARPS = 4)
     const PrefixHead head = *a.head;
     if (head.total < 0) return;
-    const int seq = sequence_of(a.row_offsets, a.seqs, token, lane);
-    int of[2] = {0, a.own.seqs > 0 ? a.prefix.seqs + seq : -1};
-    if (a.seq_offsets != nullptr)
-        of[0] = seq < a.seq_offsets[0] || seq >= a.seq_offsets[a.prefix.seqs] ? -1 : sequence_of(a.seq_offsets, a.prefix.seqs, seq, lane);
-    const int kv = qh / a.group, g = qh - kv * a.group;
-    // stored row of the first piece of either entry, and the number of pieces
-    long long at[2] = {0, 0};
-    int parts[2] = {0, 0};
-    for (int which = 0; which < 2; which++) {
-        if (of[which] < 0 || head.share == 0) continue;
-        const PrefixEntry e = a.entries[of[which]];
-        if (e.units == 0 || token < e.first || token >= e.first + e.tokens) continue;      // (offsets that go up and down)
-        const int in = (int)(token - e.first), block = in / (alternates<DIM>(a, e) ? a.block_tokens : 2 * a.block_tokens);
-        const long long s0 = e.step0 + ((long long)kv * e.blocks + block) * e.units;
-        const long long c0 = s0 / head.share, c1 = (s0 + e.units - 1) / head.share;
-        at[which] = c0 * PrefixShape<DIM>::STORE + e.row0 + ((long long)kv * e.tokens + in) * a.group + g;
-        parts[which] = (int)(c1 - c0) + 1;
-    }
-    auto row_of = [&](int i) { return i < parts[0] ? at[0] + (long long)i * PrefixShape<DIM>::STORE : at[1] + (long long)(i - parts[0]) * PrefixShape<DIM>::STORE; };
-    const int n = parts[0] + parts[1];
-    float top = -INFINITY;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, a.stats[row_of(i)].x);
+    const uint32_t per_kv = (uint32_t)a.rows * a.group, blocks = (per_kv + kJoinRows - 1) / kJoinRows;     // (below 2^31)
+    const uint32_t kv = blockIdx.x / blocks, row0 = (blockIdx.x - kv * blocks) * kJoinRows;
+    for (int k = warp; k < kJoinRows; k += WARPS) {
+        const uint32_t token = (row0 + k) / (uint32_t)a.group;
+        const int g = (int)(row0 + k - token * a.group);
+        Row r = {};
+        bool used = row0 + k < per_kv && token >= a.row_offsets[0] && token < a.row_offsets[a.seqs];
+        if (used) {
+            const int seq = sequence_of(a.row_offsets, a.seqs, token, lane);
+            int of[2] = {0, a.own.seqs > 0 ? a.prefix.seqs + seq : -1};
+            if (a.seq_offsets != nullptr)
+                of[0] = seq < a.seq_offsets[0] || seq >= a.seq_offsets[a.prefix.seqs] ? -1 : sequence_of(a.seq_offsets, a.prefix.seqs, seq, lane);
+            long long at[2] = {0, 0};                           // stored row of the first piece
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float total = 0.0f, acc[PER];
+            for (int which = 0; which < 2; which++) {
+                if (of[which] < 0 || head.share == 0) continue;
+                const PrefixEntry e = a.entries[of[which]];
+                if (e.units == 0 || token < e.first || token >= e.first + e.tokens) continue;      // (offsets that go up and down)
+                const int in = (int)(token - e.first), set = in / a.block_tokens, block = alternates<DIM>(a, e) ? set : set >> 1;
+                const long long s0 = e.step0 + ((long long)kv * e.blocks + block) * e.units;
+                const long long c0 = quotient(s0, head.share), c1 = quotient(s0 + e.units - 1, head.share);
+                const long long first = c0 * PrefixShape<DIM>::STORE + e.row0 + ((long long)kv * e.tokens + (long long)set * a.block_tokens) * a.group;
+                const int row = (in - set * a.block_tokens) * a.group + g;
+                at[which] = first + row;
+                r.from[which] = reinterpret_cast<const float4*>(a.partial + first * DIM) + row;
+                r.rows[which] = min(a.block_tokens, e.tokens - set * a.block_tokens) * a.group;
+                r.parts[which] = (int)(c1 - c0) + 1;
+            }
+            const int n = r.parts[0] + r.parts[1];
+            auto stat = [&](int i) {
+                return i >= n ? make_float2(-INFINITY, 0.0f)
+                              : a.stats[i < r.parts[0] ? at[0] + (long long)i * PrefixShape<DIM>::STORE : at[1] + (long long)(i - r.parts[0]) * PrefixShape<DIM>::STORE];
+            };
+            const float2 mine = stat(lane);                     // (all of them, unless the row is cut into more than 32)
+            float top = mine.x;
+            for (int i = lane + 32; i < n; i += 32) top = fmaxf(top, stat(i).x);
 #pragma unroll
-    for (int i = 0; i < PER; i++) acc[i] = 0.0f;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        // a lane looks after one piece's m and l
-        float2 s = make_float2(-INFINITY, 0.0f);
-        if (i0 + lane < n) s = a.stats[row_of(i0 + lane)];
-        const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - top);
-        total += weight * s.y;
-        const int m = min(32, n - i0);
-        for (int k0 = warp; k0 < m; k0 += WARPS * AHEAD) {
-            float o[AHEAD][PER], f[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; u++) {
-                const int k = k0 + u * WARPS;
-                f[u] = k < m ? __shfl_sync(0xffffffffu, weight, k) : 0.0f;
-                const float* from = a.partial + row_of(i0 + k) * DIM + lane * PER;
-                if (f[u] == 0.0f) {                             // (a piece without tiles stored no O)
-#pragma unroll
-                    for (int c = 0; c < PER; c++) o[u][c] = 0.0f;
-                } else if constexpr (PER == 2) {
-                    const float2 x = *reinterpret_cast<const float2*>(from);
-                    o[u][0] = x.x; o[u][1] = x.y;
-                } else {
-#pragma unroll
-                    for (int c = 0; c < PER; c += 4) {
-                        const float4 x = *reinterpret_cast<const float4*>(from + c);
-                        o[u][c] = x.x; o[u][c + 1] = x.y; o[u][c + 2] = x.z; o[u][c + 3] = x.w;
-                    }
-                }
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            float total = 0.0f;
+            for (int i = lane; i < n; i += 32) {
+                const float2 s = i < 32 ? mine : stat(i);
+                const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - top);
+                weights[k][i] = weight;
+                total += weight * s.y;
             }
 #pragma unroll
-            for (int u = 0; u < AHEAD; u++)
-#pragma unroll
-                for (int c = 0; c < PER; c++) acc[c] += f[u] * o[u][c];
+            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            r.inv = total == 0.0f ? 0.0f : 1.0f / total;
+            if (a.lse != nullptr && lane == 0) a.lse[(long long)token * a.q_heads + kv * a.group + g] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+        }
+        if (lane == 0) {
+            if (!used) r.parts[0] = -1;
+            found[k] = r;
         }
     }
+    __syncthreads();
+    const int k = threadIdx.x % kJoinRows, chunk = threadIdx.x / kJoinRows;
+    const Row r = found[k];
+    if (r.parts[0] < 0) return;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float4 *const from0 = r.from[0] + (long long)chunk * r.rows[0], *const from1 = r.from[1] + (long long)chunk * r.rows[1];
+    const int n = r.parts[0] + r.parts[1];
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        float4 o[AHEAD];
+        float f[AHEAD];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if constexpr (WARPS > 1) {
-        __shared__ float parked[WARPS - 1][DIM];
-        if (warp > 0)
+        for (int u = 0; u < AHEAD; u++) {
+            const int i = i0 + u;
+            f[u] = i < n ? weights[k][i] : 0.0f;
+            o[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            // (a piece without tiles has the weight 0: it stored no O)
+            if (f[u] != 0.0f) o[u] = i < r.parts[0] ? from0[(long long)i * (PrefixShape<DIM>::STORE * (DIM / 4))] : from1[(long long)(i - r.parts[0]) * (PrefixShape<DIM>::STORE * (DIM / 4))];
+        }
 #pragma unroll
-            for (int c = 0; c < PER; c++) parked[warp - 1][c * 32 + lane] = acc[c];
-        __syncthreads();
-        if (warp > 0) return;
-#pragma unroll
-        for (int k = 0; k < WARPS - 1; k++)
-#pragma unroll
-            for (int c = 0; c < PER; c++) acc[c] += parked[k][c * 32 + lane];
+        for (int u = 0; u < AHEAD; u++) {
+            acc.x += f[u] * o[u].x;
+            acc.y += f[u] * o[u].y;
+            acc.z += f[u] * o[u].z;
+            acc.w += f[u] * o[u].w;
+        }
     }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (token * a.q_heads + qh) * DIM + lane * PER);
-#pragma unroll
-    for (int c = 0; c < PER; c += 2) to[c / 2] = Pair<T>::pack(acc[c] * inv, acc[c + 1] * inv);
-    if (a.lse != nullptr && lane == 0) a.lse[token * a.q_heads + qh] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+    const uint32_t token = (row0 + k) / (uint32_t)a.group;
+    const int g = (int)(row0 + k - token * a.group);
+    *reinterpret_cast<uint2*>(a.out + ((long long)token * a.q_heads + kv * a.group + g) * DIM + chunk * 4) =
+        make_uint2(Pair<T>::pack(acc.x * r.inv, acc.y * r.inv), Pair<T>::pack(acc.z * r.inv, acc.w * r.inv));
 }
 
 }  // namespace sttm

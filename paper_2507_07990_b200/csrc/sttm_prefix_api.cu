@@ -13,7 +13,6 @@ using namespace sttm;
 
 struct PrefixPlan {
     long long grid, join_grid;
-    int join_warps;                             // per row and query head
     size_t entries, stats, partial, total;      // byte offsets in the workspace, and its size
 };
 
@@ -30,11 +29,10 @@ sttm_status plan_prefix(const sttm_cache* prefix, const sttm_cache* own, const s
     const int group = p->q_heads / prefix->heads;
     if (group > 64 || p->max_prefix > kMaxSlots || (own != nullptr && p->max_own > kMaxSlots)) return STTM_ERR_UNSUPPORTED;
     if (p->rows > INT_MAX - 256 || p->seqs > INT_MAX / 2 || prefix->seqs > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
-    pl->grid = sm_count();
+    pl->grid = std::min(sm_count(), kJoinParts / 2);
     const long long heads = p->rows * p->q_heads;
-    pl->join_warps = heads <= pl->grid * 16 ? 4 : 1;
-    pl->join_grid = (heads * pl->join_warps + kPrefixJoinThreads / 32 - 1) / (kPrefixJoinThreads / 32);
-    if (pl->join_grid > INT_MAX) return STTM_ERR_UNSUPPORTED;
+    pl->join_grid = (p->rows * group + kJoinRows - 1) / kJoinRows * prefix->heads;
+    if (heads > INT_MAX) return STTM_ERR_UNSUPPORTED;
     // every row once per kind of entry, and every CTA's pieces in a stretch of their own
     const long long rows = pl->grid * 256 + heads * (own != nullptr ? 2 : 1);
     pl->entries = 256;
@@ -137,8 +135,7 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
         static size_t allowed[kMaxDevices] = {};
         if ((r = allow_smem((const void*)k_prefix_attend<T, D>, PrefixShape<D>::SMEM, allowed)) != STTM_OK) return r;
         if ((r = launch(k_prefix_attend<T, D>, pl.grid, PrefixShape<D>::THREADS, PrefixShape<D>::SMEM, 0, stream, a, maps)) != STTM_OK) return r;
-        return pl.join_warps == 4 ? launch(k_prefix_join<T, D, 4>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a)
-                                  : launch(k_prefix_join<T, D, 1>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a);
+        return launch(k_prefix_join<T, D>, pl.join_grid, kPrefixJoinThreads<D>, 0, 0, stream, a);
     });
 }
 
