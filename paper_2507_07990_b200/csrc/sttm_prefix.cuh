@@ -41,6 +41,7 @@ struct PrefixArgs {
     int32_t* status;
     struct PrefixHead* head;      // workspace
     struct PrefixEntry* entries;
+    int32_t *own_of, *prefix_of;  // [rows] a token's entries
     float2* stats;                // per stored row: m (times c, in powers of two) and l
     float* partial;               // O of the stored rows: per block of rows [dim / 4][rows][4]
 };
@@ -396,6 +397,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == COPY_WARP && lane < 5) {                        // (the maps are parameters: no kernel before writes them)
+        const CUtensorMap* const map[5] = {&maps.q, &maps.k[0], &maps.v[0], &maps.k[1], &maps.v[1]};
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane == 0 ? map[0] : lane == 1 ? map[1] : lane == 2 ? map[2] : lane == 3 ? map[3] : map[4])) : "memory");
+    }
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_word)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -407,66 +412,69 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     wait_for_prior_kernel();
     let_next_kernel_start();
 
-    // ---- shares: the sum of all entries' steps, then the entry in which this CTA's first step lies ----
+    // ---- shares: the sum of all entries' steps, and the entry in which this CTA's first step lies ----
     const int entries = a.prefix.seqs + a.own.seqs;
     int32_t bits = 0;
-    long long mine = 0;
-    for (int e = tid; e < entries; e += Shape::THREADS) {
-        const PrefixEntry x = prefix_entry<DIM>(a, e, bits);
-        mine += steps_of(a, x);
-    }
-    mine = warp_scan(mine, lane);
-    if (lane == 31) scan[warp] = mine;
-    const int bad = __syncthreads_or(bits & kStatusArg);
+    PrefixEntry x = {};                                         // this thread's entry of a go, with what is before it
+    long long steps = 0, rows = 0;                              // of the goes so far
+    auto go_through = [&](int e0) {
+        const int e = e0 + tid;
+        x = PrefixEntry{};
+        if (e < entries) x = prefix_entry<DIM>(a, e, bits);
+        const long long s = steps_of(a, x), r = rows_of(a, x), si = warp_scan(s, lane), ri = warp_scan(r, lane);
+        if (e0 > 0) __syncthreads();                            // (scan has been read)
+        if (lane == 31) {
+            scan[warp] = si;
+            scan[16 + warp] = ri;
+        }
+        const int bad = __syncthreads_or(bits & kStatusArg);
+        x.step0 = steps + si - s;
+        x.row0 = rows + ri - r;
+        for (int w = 0; w < WARPS; w++) {
+            const long long sw = scan[w], rw = scan[16 + w];
+            if (w < warp) {
+                x.step0 += sw;
+                x.row0 += rw;
+            }
+            steps += sw;
+            rows += rw;
+        }
+        return bad;
+    };
+    int bad = 0;
+    for (int e0 = 0; e0 < entries; e0 += Shape::THREADS) bad |= go_through(e0);
     if (blockIdx.x == 0 && bits) raise_status(a.status, bits);
-    long long total = 0;
-    for (int w = 0; w < WARPS; w++) total += scan[w];
-    if (bad) total = 0;
-    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    const long long total = bad ? 0 : steps, share = quotient(total + gridDim.x - 1, gridDim.x);
     if (blockIdx.x == 0 && tid == 0) *a.head = PrefixHead{bad ? -1 : total, share};
     PieceWalk<DIM> walk;
     walk.step = min(total, (long long)blockIdx.x * share);
     walk.end = min(total, walk.step + share);
-    if (walk.step < walk.end) {
-        long long steps = 0, rows = 0;                          // before the entries of this go
+    if (total > 0) {
         PrefixEntry* found = reinterpret_cast<PrefixEntry*>(scan + 40);
         int* found_at = reinterpret_cast<int*>(scan + 48);
+        const bool once = entries <= Shape::THREADS;            // x is still there
+        steps = rows = 0;
         for (int e0 = 0; e0 < entries; e0 += Shape::THREADS) {
+            if (!once) {
+                __syncthreads();
+                go_through(e0);
+            }
             const int e = e0 + tid;
-            PrefixEntry x = {};
-            long long s = 0, r = 0;
-            if (e < entries) {
-                x = prefix_entry<DIM>(a, e, bits);
-                s = steps_of(a, x);
-                r = rows_of(a, x);
-            }
-            const long long si = warp_scan(s, lane), ri = warp_scan(r, lane);
-            __syncthreads();
-            if (lane == 31) {
-                scan[warp] = si;
-                scan[16 + warp] = ri;
-            }
-            __syncthreads();
-            x.step0 = steps + si - s;
-            x.row0 = rows + ri - r;
-            for (int w = 0; w < WARPS; w++) {
-                if (w < warp) {
-                    x.step0 += scan[w];
-                    x.row0 += scan[16 + w];
-                }
-                steps += scan[w];
-                rows += scan[16 + w];
-            }
-            if (e < entries && s > 0 && x.step0 <= walk.step && walk.step < x.step0 + s) {
+            if (e < entries && x.step0 <= walk.step && walk.step < x.step0 + steps_of(a, x)) {
                 *found = x;
                 *found_at = e;
             }
             if (blockIdx.x == 0 && e < entries) a.entries[e] = x;
-            if (blockIdx.x != 0 && steps > walk.step) break;    // (the same for the whole CTA)
+            // the tokens' entries, shared between the CTAs (one does it where entries are so many that the others do not see them all)
+            if (e < entries && x.units > 0 && (once || blockIdx.x == 0))
+                for (int i = once ? blockIdx.x : 0; i < x.tokens; i += once ? gridDim.x : 1) (e < a.prefix.seqs ? a.prefix_of : a.own_of)[x.first + i] = e;
+            if (blockIdx.x != 0 && !once && steps > walk.step) break;       // (the same for the whole CTA)
         }
         __syncthreads();
-        walk.e = *found;
-        walk.at = *found_at;
+        if (walk.step < walk.end) {
+            walk.e = *found;
+            walk.at = *found_at;
+        }
     }
 
     // 384 threads are launched with 168 registers each (64512).  The softmax warps hold a row of 128 logits: they take 208, for
@@ -861,115 +869,115 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
 
 // ---- pieces of a row to its output ----
 
-constexpr int kJoinRows = 8;                                    // rows (token, query head of one KV head) per block
+constexpr int kPrefixJoinThreads = 256;
 constexpr int kJoinParts = 320;                                 // pieces of a row at most: two entries' over all CTAs
 
-template <int DIM>
-constexpr int kPrefixJoinThreads = kJoinRows * DIM / 4;
-
-// A block puts eight rows together; its threads take four channels of a row each, rows beside each other as the pieces store them.
-// First a warp per row finds the row's pieces and their weights.
-template <typename T, int DIM>
-__global__ void __launch_bounds__(kPrefixJoinThreads<DIM>) k_prefix_join(const __grid_constant__ PrefixArgs a) {
-    constexpr int WARPS = kPrefixJoinThreads<DIM> / 32, AHEAD = 8;
+// A block puts ROWS rows (token, query head of one KV head) together: 8 where rows are few and their pieces many, else 32.  First a part
+// of a warp per row finds the row's pieces and their weights; then a thread takes four channels of a row, rows beside each
+// other as the pieces store them.
+template <typename T, int DIM, int ROWS>
+__global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid_constant__ PrefixArgs a) {
+    constexpr int LANES = kPrefixJoinThreads / ROWS;            // per row
+    constexpr int AHEAD = ROWS == 8 ? 16 : 8;
     struct Row {
         const float4* from[2];    // the row's first four channels in its first piece
         int parts[2], rows[2];    // pieces; rows of the block that they lie in
-        float inv;
+        float inv, top;
     };
-    __shared__ Row found[kJoinRows];
-    __shared__ float weights[kJoinRows][kJoinParts];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ Row found[ROWS];
+    __shared__ float weights[ROWS][kJoinParts + 1];             // (rows in different banks)
     wait_for_prior_kernel();
     let_next_kernel_start();
-    const PrefixHead head = *a.head;
-    if (head.total < 0) return;
-    const uint32_t per_kv = (uint32_t)a.rows * a.group, blocks = (per_kv + kJoinRows - 1) / kJoinRows;     // (below 2^31)
-    const uint32_t kv = blockIdx.x / blocks, row0 = (blockIdx.x - kv * blocks) * kJoinRows;
-    for (int k = warp; k < kJoinRows; k += WARPS) {
+    const uint32_t per_kv = (uint32_t)a.rows * a.group, blocks = (per_kv + ROWS - 1) / ROWS;       // (below 2^31)
+    const uint32_t kv = blockIdx.x / blocks, row0 = (blockIdx.x - kv * blocks) * ROWS;
+    {
+        const int k = threadIdx.x / LANES, lane = threadIdx.x % LANES;
         const uint32_t token = (row0 + k) / (uint32_t)a.group;
         const int g = (int)(row0 + k - token * a.group);
         Row r = {};
-        bool used = row0 + k < per_kv && token >= a.row_offsets[0] && token < a.row_offsets[a.seqs];
-        if (used) {
-            const int seq = sequence_of(a.row_offsets, a.seqs, token, lane);
-            int of[2] = {0, a.own.seqs > 0 ? a.prefix.seqs + seq : -1};
-            if (a.seq_offsets != nullptr)
-                of[0] = seq < a.seq_offsets[0] || seq >= a.seq_offsets[a.prefix.seqs] ? -1 : sequence_of(a.seq_offsets, a.prefix.seqs, seq, lane);
-            long long at[2] = {0, 0};                           // stored row of the first piece
+        // (a token of no sequence, or without a prefix, finds rubbish in the tables: an entry whose tokens it is not among)
+        const bool there = row0 + k < per_kv;
+        const int of[2] = {there ? a.prefix_of[token] : -1, there && a.own.seqs > 0 ? a.own_of[token] : -1};
+        const bool used = there && token >= a.row_offsets[0] && token < a.row_offsets[a.seqs];
+        const PrefixHead head = *a.head;
+        long long at[2] = {0, 0};                               // stored row of the first piece
 #pragma unroll
-            for (int which = 0; which < 2; which++) {
-                if (of[which] < 0 || head.share == 0) continue;
-                const PrefixEntry e = a.entries[of[which]];
-                if (e.units == 0 || token < e.first || token >= e.first + e.tokens) continue;      // (offsets that go up and down)
-                const int in = (int)(token - e.first), set = in / a.block_tokens, block = alternates<DIM>(a, e) ? set : set >> 1;
-                const long long s0 = e.step0 + ((long long)kv * e.blocks + block) * e.units;
-                const long long c0 = quotient(s0, head.share), c1 = quotient(s0 + e.units - 1, head.share);
-                const long long first = c0 * PrefixShape<DIM>::STORE + e.row0 + ((long long)kv * e.tokens + (long long)set * a.block_tokens) * a.group;
-                const int row = (in - set * a.block_tokens) * a.group + g;
-                at[which] = first + row;
-                r.from[which] = reinterpret_cast<const float4*>(a.partial + first * DIM) + row;
-                r.rows[which] = min(a.block_tokens, e.tokens - set * a.block_tokens) * a.group;
-                r.parts[which] = (int)(c1 - c0) + 1;
-            }
-            const int n = r.parts[0] + r.parts[1];
-            auto stat = [&](int i) {
-                return i >= n ? make_float2(-INFINITY, 0.0f)
-                              : a.stats[i < r.parts[0] ? at[0] + (long long)i * PrefixShape<DIM>::STORE : at[1] + (long long)(i - r.parts[0]) * PrefixShape<DIM>::STORE];
-            };
-            const float2 mine = stat(lane);                     // (all of them, unless the row is cut into more than 32)
-            float top = mine.x;
-            for (int i = lane + 32; i < n; i += 32) top = fmaxf(top, stat(i).x);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            float total = 0.0f;
-            for (int i = lane; i < n; i += 32) {
-                const float2 s = i < 32 ? mine : stat(i);
-                const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - top);
-                weights[k][i] = weight;
-                total += weight * s.y;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            r.inv = total == 0.0f ? 0.0f : 1.0f / total;
-            if (a.lse != nullptr && lane == 0) a.lse[(long long)token * a.q_heads + kv * a.group + g] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+        for (int which = 0; which < 2; which++) {
+            const bool fits = used && head.total > 0 && of[which] >= (which ? a.prefix.seqs : 0) && of[which] < a.prefix.seqs + (which ? a.own.seqs : 0);
+            if (!fits) continue;
+            const PrefixEntry e = a.entries[of[which]];
+            if (e.units == 0 || token < e.first || token >= e.first + e.tokens) continue;
+            const int in = (int)(token - e.first), set = in / a.block_tokens, block = alternates<DIM>(a, e) ? set : set >> 1;
+            const long long s0 = e.step0 + ((long long)kv * e.blocks + block) * e.units;
+            const long long c0 = quotient(s0, head.share), c1 = quotient(s0 + e.units - 1, head.share);
+            const long long first = c0 * PrefixShape<DIM>::STORE + e.row0 + ((long long)kv * e.tokens + (long long)set * a.block_tokens) * a.group;
+            const int row = (in - set * a.block_tokens) * a.group + g;
+            at[which] = first + row;
+            r.from[which] = reinterpret_cast<const float4*>(a.partial + first * DIM) + row;
+            r.rows[which] = min(a.block_tokens, e.tokens - set * a.block_tokens) * a.group;
+            r.parts[which] = (int)(c1 - c0) + 1;
         }
+        const int n = r.parts[0] + r.parts[1];
+        auto stat = [&](int i) {
+            return i >= n ? make_float2(-INFINITY, 0.0f)
+                          : a.stats[i < r.parts[0] ? at[0] + (long long)i * PrefixShape<DIM>::STORE : at[1] + (long long)(i - r.parts[0]) * PrefixShape<DIM>::STORE];
+        };
+        const float2 mine = stat(lane);                         // (all of them, unless the row is cut into more than LANES)
+        r.top = mine.x;
+        for (int i = lane + LANES; i < n; i += LANES) r.top = fmaxf(r.top, stat(i).x);
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
+        float total = 0.0f;
+        for (int i = lane; i < n; i += LANES) {
+            const float2 s = i < LANES ? mine : stat(i);
+            const float weight = s.x == -INFINITY ? 0.0f : exp2f(s.x - r.top);
+            weights[k][i] = weight;
+            total += weight * s.y;
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        r.inv = total == 0.0f ? 0.0f : 1.0f / total;
+        if (!used || head.total < 0) r.parts[0] = -1;           // (bad offsets: nothing is written)
         if (lane == 0) {
-            if (!used) r.parts[0] = -1;
             found[k] = r;
+            if (r.parts[0] >= 0 && a.lse != nullptr)
+                a.lse[(long long)token * a.q_heads + kv * a.group + g] = total == 0.0f ? -INFINITY : (r.top + log2f(total)) * 0.69314718055994531f;
         }
     }
     __syncthreads();
-    const int k = threadIdx.x % kJoinRows, chunk = threadIdx.x / kJoinRows;
+    const int k = threadIdx.x % ROWS;
     const Row r = found[k];
     if (r.parts[0] < 0) return;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const float4 *const from0 = r.from[0] + (long long)chunk * r.rows[0], *const from1 = r.from[1] + (long long)chunk * r.rows[1];
     const int n = r.parts[0] + r.parts[1];
-#pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += AHEAD) {
-        float4 o[AHEAD];
-        float f[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; u++) {
-            const int i = i0 + u;
-            f[u] = i < n ? weights[k][i] : 0.0f;
-            o[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            // (a piece without tiles has the weight 0: it stored no O)
-            if (f[u] != 0.0f) o[u] = i < r.parts[0] ? from0[(long long)i * (PrefixShape<DIM>::STORE * (DIM / 4))] : from1[(long long)(i - r.parts[0]) * (PrefixShape<DIM>::STORE * (DIM / 4))];
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; u++) {
-            acc.x += f[u] * o[u].x;
-            acc.y += f[u] * o[u].y;
-            acc.z += f[u] * o[u].z;
-            acc.w += f[u] * o[u].w;
-        }
-    }
     const uint32_t token = (row0 + k) / (uint32_t)a.group;
-    const int g = (int)(row0 + k - token * a.group);
-    *reinterpret_cast<uint2*>(a.out + ((long long)token * a.q_heads + kv * a.group + g) * DIM + chunk * 4) =
-        make_uint2(Pair<T>::pack(acc.x * r.inv, acc.y * r.inv), Pair<T>::pack(acc.z * r.inv, acc.w * r.inv));
+    uint16_t* const out = a.out + ((long long)token * a.q_heads + kv * a.group + (row0 + k - token * a.group)) * DIM;
+#pragma unroll 1
+    for (int chunk = threadIdx.x / ROWS; chunk < DIM / 4; chunk += LANES) {
+        const float4 *const from0 = r.from[0] + (long long)chunk * r.rows[0], *const from1 = r.from[1] + (long long)chunk * r.rows[1];
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+        for (int i0 = 0; i0 < n; i0 += AHEAD) {
+            float4 o[AHEAD];
+            float f[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) {
+                const int i = i0 + u;
+                f[u] = i < n ? weights[k][i] : 0.0f;
+                o[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                // (a piece without tiles has the weight 0: it stored no O)
+                if (f[u] != 0.0f)
+                    o[u] = i < r.parts[0] ? from0[(long long)i * (PrefixShape<DIM>::STORE * (DIM / 4))] : from1[(long long)(i - r.parts[0]) * (PrefixShape<DIM>::STORE * (DIM / 4))];
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) {
+                acc.x += f[u] * o[u].x;
+                acc.y += f[u] * o[u].y;
+                acc.z += f[u] * o[u].z;
+                acc.w += f[u] * o[u].w;
+            }
+        }
+        *reinterpret_cast<uint2*>(out + chunk * 4) = make_uint2(Pair<T>::pack(acc.x * r.inv, acc.y * r.inv), Pair<T>::pack(acc.z * r.inv, acc.w * r.inv));
+    }
 }
 
 }  // namespace sttm

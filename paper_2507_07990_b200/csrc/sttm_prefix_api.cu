@@ -13,7 +13,8 @@ using namespace sttm;
 
 struct PrefixPlan {
     long long grid, join_grid;
-    size_t entries, stats, partial, total;      // byte offsets in the workspace, and its size
+    int join_rows;                              // per block
+    size_t entries, of, stats, partial, total;  // byte offsets in the workspace, and its size
 };
 
 sttm_status plan_prefix(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p, PrefixPlan* pl) {
@@ -31,12 +32,14 @@ sttm_status plan_prefix(const sttm_cache* prefix, const sttm_cache* own, const s
     if (p->rows > INT_MAX - 256 || p->seqs > INT_MAX / 2 || prefix->seqs > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
     pl->grid = std::min(sm_count(), kJoinParts / 2);
     const long long heads = p->rows * p->q_heads;
-    pl->join_grid = (p->rows * group + kJoinRows - 1) / kJoinRows * prefix->heads;
+    pl->join_rows = heads <= pl->grid * 32 ? 8 : 32;
+    pl->join_grid = (p->rows * group + pl->join_rows - 1) / pl->join_rows * prefix->heads;
     if (heads > INT_MAX) return STTM_ERR_UNSUPPORTED;
     // every row once per kind of entry, and every CTA's pieces in a stretch of their own
     const long long rows = pl->grid * 256 + heads * (own != nullptr ? 2 : 1);
     pl->entries = 256;
-    pl->stats = pl->entries + align_up(((size_t)prefix->seqs + (own != nullptr ? own->seqs : 0)) * sizeof(PrefixEntry));
+    pl->of = pl->entries + align_up(((size_t)prefix->seqs + (own != nullptr ? own->seqs : 0)) * sizeof(PrefixEntry));
+    pl->stats = pl->of + 2 * align_up((size_t)p->rows * 4);
     pl->partial = pl->stats + align_up((size_t)rows * sizeof(float2));
     pl->total = pl->partial + align_up((size_t)rows * prefix->dim * 4);
     return STTM_OK;
@@ -119,6 +122,8 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
     a.status = p->device_status;
     a.head = (PrefixHead*)w;
     a.entries = (PrefixEntry*)(w + pl.entries);
+    a.prefix_of = (int32_t*)(w + pl.of);
+    a.own_of = (int32_t*)(w + pl.of + align_up((size_t)p->rows * 4));
     a.stats = (float2*)(w + pl.stats);
     a.partial = (float*)(w + pl.partial);
     return by_type(prefix, [&](auto tag, auto dim) -> sttm_status {
@@ -135,7 +140,8 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
         static size_t allowed[kMaxDevices] = {};
         if ((r = allow_smem((const void*)k_prefix_attend<T, D>, PrefixShape<D>::SMEM, allowed)) != STTM_OK) return r;
         if ((r = launch(k_prefix_attend<T, D>, pl.grid, PrefixShape<D>::THREADS, PrefixShape<D>::SMEM, 0, stream, a, maps)) != STTM_OK) return r;
-        return launch(k_prefix_join<T, D>, pl.join_grid, kPrefixJoinThreads<D>, 0, 0, stream, a);
+        return pl.join_rows == 8 ? launch(k_prefix_join<T, D, 8>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a)
+                                 : launch(k_prefix_join<T, D, 32>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a);
     });
 }
 
