@@ -53,16 +53,20 @@ MatmulPlan plan_matmul(const sttm_matmul_params* p) {
     pl.nt = 256;
     if (pl.swap)
         for (pl.nt = 16; pl.nt < p->rows;) pl.nt *= 2;
-    const long long a_rows = pl.swap ? p->outer : p->rows, b_rows = pl.swap ? p->rows : p->outer;
-    pl.a_tiles = (a_rows + 127) / 128;
-    pl.b_tiles = (b_rows + pl.nt - 1) / pl.nt;
+    pl.a_tiles = pl.swap ? (p->outer + 127) / 128 : (p->rows + 255) / 256;
+    pl.b_tiles = pl.swap ? (p->rows + pl.nt - 1) / pl.nt : ((long long)p->outer + 255) / 256;
     const long long tiles = pl.a_tiles * pl.b_tiles;
+    if (!pl.swap) {
+        pl.cluster = 2;
+        pl.stages = kPairStages;
+        pl.grid = 2 * std::min<long long>(tiles, sms / 2);
+        return pl;
+    }
     // two CTAs to an SM where their rings and accumulators fit
     const int per_sm = pl.nt <= 64 ? 2 : 1;
     pl.stages = std::min(kMatMaxStages, (int)((227 * 1024 / per_sm - 1024 - matmul_fixed_bytes()) / matmul_slot(pl.nt)));
     pl.cluster = 1;
-    if (pl.swap)
-        while (pl.cluster < 8 && tiles * pl.cluster * 2 <= (long long)sms * per_sm && blocks >= 4 * pl.cluster) pl.cluster *= 2;
+    while (pl.cluster < 8 && tiles * pl.cluster * 2 <= (long long)sms * per_sm && blocks >= 4 * pl.cluster) pl.cluster *= 2;
     pl.grid = pl.cluster > 1 ? tiles * pl.cluster : std::min<long long>(tiles, (long long)sms * per_sm);
     return pl;
 }
@@ -78,12 +82,12 @@ sttm_status make_rows_map(const void* base, long long rows, int inner, long long
     return r == CUDA_SUCCESS ? STTM_OK : STTM_ERR_UNSUPPORTED;
 }
 
-template <typename T, int NT, bool SWAP>
+template <typename T, int NT>
 sttm_status launch_matmul(const MatmulArgs& a, const MatmulPlan& pl, const CUtensorMap& ma, const CUtensorMap& mb, void* stream) {
     static size_t allowed[kMaxDevices] = {};
     const size_t smem = (size_t)pl.stages * matmul_slot(NT) + matmul_fixed_bytes();
-    const sttm_status s = allow_smem((const void*)k_quant_matmul<T, NT, SWAP>, smem, allowed);
-    return s != STTM_OK ? s : launch(k_quant_matmul<T, NT, SWAP>, pl.grid, kMatThreads, smem, pl.cluster > 1 ? pl.cluster : 0, stream, a, ma, mb);
+    const sttm_status s = allow_smem((const void*)k_quant_matmul<T, NT>, smem, allowed);
+    return s != STTM_OK ? s : launch(k_quant_matmul<T, NT>, pl.grid, kMatThreads, smem, pl.cluster > 1 ? pl.cluster : 0, stream, a, ma, mb);
 }
 
 // Do two arrays of `rows` rows share memory, other than one in the other's place?
@@ -192,16 +196,20 @@ sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream) {
     CUtensorMap mx, mw;
     sttm_status s;
     if ((s = make_rows_map(p->x, p->rows, p->inner, p->x_row, pl.swap ? pl.nt : 128, &mx)) != STTM_OK) return s;
-    if ((s = make_rows_map(p->w, p->outer, p->inner, p->w_row, pl.swap ? 128 : pl.nt, &mw)) != STTM_OK) return s;
+    if ((s = make_rows_map(p->w, p->outer, p->inner, p->w_row, 128, &mw)) != STTM_OK) return s;
     return by_element(p->out_dtype, [&](auto tag) -> sttm_status {
         using T = decltype(tag);
-        if (!pl.swap) return launch_matmul<T, 256, false>(a, pl, mx, mw, stream);
+        if (!pl.swap) {
+            static size_t allowed[kMaxDevices] = {};
+            const sttm_status r = allow_smem((const void*)k_quant_matmul_pair<T>, kPairSmem, allowed);
+            return r != STTM_OK ? r : launch(k_quant_matmul_pair<T>, pl.grid, kMatThreads, kPairSmem, 2, stream, a, mx, mw);
+        }
         switch (pl.nt) {
-            case 16: return launch_matmul<T, 16, true>(a, pl, mw, mx, stream);
-            case 32: return launch_matmul<T, 32, true>(a, pl, mw, mx, stream);
-            case 64: return launch_matmul<T, 64, true>(a, pl, mw, mx, stream);
-            case 128: return launch_matmul<T, 128, true>(a, pl, mw, mx, stream);
-            default: return launch_matmul<T, 256, true>(a, pl, mw, mx, stream);
+            case 16: return launch_matmul<T, 16>(a, pl, mw, mx, stream);
+            case 32: return launch_matmul<T, 32>(a, pl, mw, mx, stream);
+            case 64: return launch_matmul<T, 64>(a, pl, mw, mx, stream);
+            case 128: return launch_matmul<T, 128>(a, pl, mw, mx, stream);
+            default: return launch_matmul<T, 256>(a, pl, mw, mx, stream);
         }
     });
 }

@@ -225,24 +225,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, ui
         ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// one lane of the warp
-__device__ __forceinline__ bool elected() {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xffffffff;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(r));
-    return r != 0;
-}
-// a value that is the same in every lane, told to the compiler
-__device__ __forceinline__ uint32_t one_value(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 // Operand whose row axis (channels) is contiguous, 128-byte swizzle: groups of eight slots 1024 bytes apart, 64-channel
 // parts `part` bytes apart.
 __device__ __forceinline__ uint64_t operand_by_n(uint32_t addr, uint32_t part) {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(part >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-constexpr uint32_t kOperandHigh = (1024 >> 4) | (1u << 14) | (2u << 29);        // the high word of both kinds
 __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -345,20 +332,6 @@ __device__ __forceinline__ void store32(float4* to, int rows, const uint32_t (&v
 #pragma unroll
     for (int i = 0; i < 8; i++)
         to[i * rows] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-}
-
-// Bounded wait of a warp for the `use`-th completion of an mbarrier of this CTA (see mbar_wait).  It polls; its acquire reaches no further than
-// the CTA: the one over a cluster costs some 200 cycles more, several times per tile.
-__device__ __forceinline__ bool mbar_wait_near(uint32_t bar, int use, bool& timed_out) {
-    const uint32_t parity = (uint32_t)(use & 1);
-    bool ok = !timed_out;
-    if (ok && !mbar_try(bar, parity)) {
-        const unsigned long long t0 = global_timer_ns();
-        while (ok && !mbar_try(bar, parity)) ok = global_timer_ns() - t0 <= kWaitLimitNs;
-    }
-    ok = __all_sync(0xffffffffu, ok);
-    timed_out = !ok;
-    return ok;
 }
 
 struct PrefixMaps {

@@ -264,4 +264,32 @@ __device__ __forceinline__ void tc_load32(uint32_t taddr, uint32_t (&v)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// the high word of the operand descriptors with 128-byte swizzle and 1024 bytes between groups of eight rows, K-major or not
+constexpr uint32_t kOperandHigh = (1024 >> 4) | (1u << 14) | (2u << 29);
+// one lane of the warp
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+// a value that is the same in every lane, told to the compiler
+__device__ __forceinline__ uint32_t one_value(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+// Bounded wait of a warp for the `use`-th completion of an mbarrier of this CTA (see mbar_wait).  It polls; its acquire reaches no further than
+// the CTA: the one over a cluster costs some 200 cycles more, several times per tile.
+__device__ __forceinline__ bool mbar_wait_near(uint32_t bar, int use, bool& timed_out) {
+    const uint32_t parity = (uint32_t)(use & 1);
+    bool ok = !timed_out;
+    if (ok && !mbar_try(bar, parity)) {
+        const unsigned long long t0 = global_timer_ns();
+        while (ok && !mbar_try(bar, parity)) ok = global_timer_ns() - t0 <= kWaitLimitNs;
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    timed_out = !ok;
+    return ok;
+}
+
 }  // namespace sttm

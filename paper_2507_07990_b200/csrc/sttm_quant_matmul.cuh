@@ -9,8 +9,8 @@
 //
 // Few tokens (SWAP): weights are the 128-row operand, tokens the NT columns; the weights' bytes bound it, and a cluster
 // shares the inner axis so that their stream is spread over all SMs.  Its CTAs put their sums into shared memory and each adds
-// up and writes every size-th token.  Many tokens: tokens are the 128 rows, NT = 256 output channels the columns, the tensor
-// cores bound it; one CTA per SM takes tile after tile, one accumulator being written out while the other fills.
+// up and writes every size-th token.  Many tokens (k_quant_matmul_pair): the tensor cores bound it; two CTAs of a cluster take 256 tokens
+// by 256 output channels together, tile after tile, one accumulator being written out while the other fills.
 #pragma once
 
 #include "sttm_cache.cuh"
@@ -75,7 +75,7 @@ __device__ __forceinline__ void tile_at(const MatmulArgs& a, int tile, int& ta, 
 template <typename T>
 __device__ __forceinline__ T narrow(float v) { return (T)v; }
 
-template <typename T, int NT, bool SWAP>
+template <typename T, int NT>
 __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_constant__ MatmulArgs a, const __grid_constant__ CUtensorMap map_a,
                                                               const __grid_constant__ CUtensorMap map_b) {
     constexpr int SLOT = matmul_slot(NT);
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
             tile_at(a, tile, ta, tb);
             if (!mbar_wait_warp(acc_full + 8 * b, n >> 1, timed_out)) break;
             tc_fence_after();
-            if constexpr (SWAP) {
+            {
                 const int ch = ta * 128 + row;
                 const float ws = ch < a.outer ? a.w_scale[ch] : 0.0f, bias = a.bias && ch < a.outer ? a.bias[ch] : 0.0f;
                 auto write = [&](int col, int sum) {
@@ -204,43 +204,13 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
                         write(col, sum);
                     }
                 }
-            } else {
-                const long long token = (long long)ta * 128 + row;
-                const float xs = token < a.rows ? a.x_scale[token] : 0.0f;
-                T* out = (T*)a.out + token * a.out_row;
-#pragma unroll 1
-                for (int c = 0; c < NT; c += 32) {
-                    uint32_t v[32];
-                    tc_load32(mine + b * NT + c, v);
-                    const int ch0 = tb * NT + c;
-                    if (token >= a.rows) continue;
-                    if (a.wide && ch0 + 32 <= a.outer) {
-                        constexpr int PER = 16 / sizeof(T);
-#pragma unroll
-                        for (int i = 0; i < 32; i += PER) {
-                            __align__(16) T piece[PER];
-#pragma unroll
-                            for (int j = 0; j < PER; j++) {
-                                const int ch = ch0 + i + j;
-                                piece[j] = narrow<T>((float)(int)v[i + j] * xs * __ldg(a.w_scale + ch) + (a.bias ? __ldg(a.bias + ch) : 0.0f));
-                            }
-                            *reinterpret_cast<uint4*>(out + ch0 + i) = *reinterpret_cast<const uint4*>(piece);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; i++) {
-                            const int ch = ch0 + i;
-                            if (ch < a.outer) out[ch] = narrow<T>((float)(int)v[i] * xs * a.w_scale[ch] + (a.bias ? a.bias[ch] : 0.0f));
-                        }
-                    }
-                }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(acc_empty + 8 * b);
         }
     }
-    if (SWAP && size > 1) {
+    if (size > 1) {
         // warps that have met at the first barrier meet at the second; every other warp, and those whose wait ran out, at both
         if (warp < 2 || n == 0) {
             cluster_arrive();
@@ -254,6 +224,195 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
     if (warp == 2) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
+    }
+    if (timed_out) raise_status(a.status, kStatusWaitTimeout);
+}
+
+// ---- many tokens ----
+
+// Two CTAs of a cluster on one tile (cta_group::2): each brings 128 of the 256 tokens and 128 of the 256 channels into its own
+// ring, the first one's issuing thread starts products that read both rings, and each CTA's tensor memory holds the sums of its own
+// 128 tokens.  Per step of 128 inner elements a CTA reads 32 KB for 512 cycles of products; a CTA alone would read 48.
+constexpr int kPairStages = 6, kPairSlot = 256 * kMatK;         // 128 rows of either operand
+constexpr size_t kPairSmem = (size_t)kPairStages * kPairSlot + (2 * kPairStages + 4) * 8 + 16 + 1024;
+constexpr int kPairGroup = 8;                                   // tiles of tokens in a row before the next tile of channels
+
+__device__ __forceinline__ void mma_i8_pair(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t accumulate) {
+    constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (32u << 17) | (16u << 24);      // as matmul_idesc: N = 256, M = 256
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 da, {%1, %3};\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(kOperandHigh), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// both CTAs' mbarriers at this place get an arrival when every product issued so far has completed
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// a tile into this CTA's memory, its bytes counted by an mbarrier of the pair's first CTA
+__device__ __forceinline__ void copy_tile_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar_cluster) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar_cluster)
+                 : "memory");
+}
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatThreads, 1)
+k_quant_matmul_pair(const __grid_constant__ MatmulArgs a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t ring = smem_u32(smem), bars = ring + kPairStages * kPairSlot;
+    const uint32_t full = bars, empty = full + 8 * kPairStages, acc_full = empty + 8 * kPairStages, acc_empty = acc_full + 16;
+    uint32_t* tmem_word = reinterpret_cast<uint32_t*>(smem + kPairStages * kPairSlot + (2 * kPairStages + 4) * 8);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster_rank();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPairStages; s++) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; b++) {
+            mbar_init(acc_full + 8 * b, 1);
+            mbar_init(acc_empty + 8 * b, 8);                    // four reading warps of either CTA
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &map_w : &map_x)) : "memory");
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_word)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_word);
+    wait_for_prior_kernel();
+    let_next_kernel_start();
+
+    const int tiles = a.a_tiles * a.b_tiles, first = blockIdx.x / 2, step = gridDim.x / 2;
+    auto place = [&](int tile, int& ta, int& tb) {
+        const int per = kPairGroup * a.b_tiles, group = tile / per, at = group * kPairGroup;
+        const int size = min(kPairGroup, a.a_tiles - at), in = tile - group * per;
+        tb = in / size;
+        ta = at + in - tb * size;
+    };
+    bool timed_out = false;
+    if (warp == 0) {
+        const uint32_t full0 = map_to_rank(full, 0);
+        uint32_t slot = 0, turn = 1, taken = 0;                 // (the first wait for every slot returns at once: the phase before the first)
+        for (int tile = first; tile < tiles && !timed_out; tile += step) {
+            int ta, tb;
+            place(tile, ta, tb);
+#pragma unroll 1
+            for (int k = 0; k < a.blocks; k++) {
+                if (!mbar_wait_near(empty + 8 * slot, turn, timed_out)) break;
+                if (lane == 0) {
+                    if (rank == 0) mbar_expect_tx(full + 8 * slot, 2 * kPairSlot);
+                    const uint32_t to = ring + slot * kPairSlot;
+                    copy_tile_pair(to, &map_x, k * kMatK, ta * 256 + rank * 128, full0 + 8 * slot);
+                    copy_tile_pair(to + 128 * kMatK, &map_w, k * kMatK, tb * 256 + rank * 128, full0 + 8 * slot);
+                }
+                __syncwarp();
+                taken++;
+                if (++slot == kPairStages) {
+                    slot = 0;
+                    turn ^= 1;
+                }
+            }
+        }
+        // The pair must not end with copies in flight: the last products that read them have completed (each CTA sees that on its own
+        // `empty`), or, where a wait ran out, the copies themselves (which the first CTA counts).
+        for (uint32_t i = taken > kPairStages ? taken - kPairStages : 0; i < taken; i++) {
+            bool late = false;
+            mbar_wait_sleep((timed_out && rank == 0 ? full : empty) + 8 * (i % kPairStages), (int)(i / kPairStages), late);
+            timed_out |= late;
+        }
+    } else if (warp == 1 && rank == 0) {
+        const uint32_t ring_lo = one_value((uint32_t)tc_operand(ring)), tm = one_value(tmem), bar = one_value(bars);
+        uint32_t slot = 0, turn = 0;
+        int n = 0;
+        for (int tile = first; tile < tiles && !timed_out; tile += step, n++) {
+            const uint32_t b = one_value(n & 1);
+            if (n >= 2 && !mbar_wait(acc_empty + 8 * b, (n >> 1) - 1, timed_out)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int k = 0; k < a.blocks; k++) {
+                const uint32_t at = one_value(slot), lo = ring_lo + at * (kPairSlot / 16), more = one_value(k > 0), last = one_value(k + 1 == a.blocks);
+                if (!mbar_wait(full + 8 * slot, turn, timed_out)) break;
+                if (elected()) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) mma_i8_pair(tm + b * 256, lo + 2 * i, lo + 128 * kMatK / 16 + 2 * i, i > 0 ? 1 : more);
+                    commit_pair(bar + 8 * kPairStages + 8 * at);
+                    if (last) commit_pair(bar + 16 * kPairStages + 8 * b);
+                }
+                __syncwarp();
+                if (++slot == kPairStages) {
+                    slot = 0;
+                    turn ^= 1;
+                }
+            }
+        }
+    } else if (warp >= 2) {
+        const int row = 32 * (warp & 3) + lane;
+        const uint32_t mine = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+        const bool weights_wide = (((uintptr_t)a.w_scale | (uintptr_t)a.bias) & 15) == 0;
+        int n = 0;
+        for (int tile = first; tile < tiles && !timed_out; tile += step, n++) {
+            const int b = n & 1;
+            int ta, tb;
+            place(tile, ta, tb);
+            const long long token = (long long)ta * 256 + rank * 128 + row;
+            const float xs = token < a.rows ? a.x_scale[token] : 0.0f;
+            T* out = (T*)a.out + token * a.out_row;
+            if (!mbar_wait_warp(acc_full + 8 * b, n >> 1, timed_out)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 256; c += 32) {
+                uint32_t v[32];
+                tc_load32(mine + b * 256 + c, v);
+                const int ch0 = tb * 256 + c;
+                if (token >= a.rows) continue;
+                if (a.wide && weights_wide && ch0 + 32 <= a.outer) {
+                    constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+                    for (int i = 0; i < 32; i += PER) {
+                        __align__(16) T piece[PER];
+#pragma unroll
+                        for (int j = 0; j < PER; j += 4) {
+                            const float4 w = __ldg(reinterpret_cast<const float4*>(a.w_scale + ch0 + i + j));
+                            const float4 o = a.bias ? __ldg(reinterpret_cast<const float4*>(a.bias + ch0 + i + j)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            piece[j] = narrow<T>((float)(int)v[i + j] * xs * w.x + o.x);
+                            piece[j + 1] = narrow<T>((float)(int)v[i + j + 1] * xs * w.y + o.y);
+                            piece[j + 2] = narrow<T>((float)(int)v[i + j + 2] * xs * w.z + o.z);
+                            piece[j + 3] = narrow<T>((float)(int)v[i + j + 3] * xs * w.w + o.w);
+                        }
+                        *reinterpret_cast<uint4*>(out + ch0 + i) = *reinterpret_cast<const uint4*>(piece);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; i++) {
+                        const int ch = ch0 + i;
+                        if (ch < a.outer) out[ch] = narrow<T>((float)(int)v[i] * xs * a.w_scale[ch] + (a.bias ? a.bias[ch] : 0.0f));
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(map_to_rank(acc_empty + 8 * b, 0));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();                                           // neither CTA ends while products may read its ring
+    cluster_wait();
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
     if (timed_out) raise_status(a.status, kStatusWaitTimeout);
 }
