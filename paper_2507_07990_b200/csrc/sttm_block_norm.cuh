@@ -33,13 +33,15 @@ struct NormArgs {
 
 constexpr int kNormMaxDim = 16384;
 
-// VEC elements in 16 bytes, or one (plain loads: an output may take the place of an input)
+// VEC elements in 16 bytes, or one.  A row's words are all on their way before the first is used, and before anything is stored: an
+// output may take the place of an input, so the compiler moves no load over a store (plain loads, for the same reason).
 template <typename T, int VEC>
 struct Elements;
 template <typename T>
 struct Elements<T, 8> {
-    static __device__ __forceinline__ void load(const T* p, float (&f)[8]) {
-        const uint4 w = *reinterpret_cast<const uint4*>(p);
+    typedef uint4 Raw;
+    static __device__ __forceinline__ Raw load(const T* p) { return *reinterpret_cast<const uint4*>(p); }
+    static __device__ __forceinline__ void split(const Raw& w, float (&f)[8]) {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -54,17 +56,16 @@ struct Elements<T, 8> {
 };
 template <>
 struct Elements<float, 4> {
-    static __device__ __forceinline__ void load(const float* p, float (&f)[4]) {
-        const float4 w = *reinterpret_cast<const float4*>(p);
-        f[0] = w.x; f[1] = w.y; f[2] = w.z; f[3] = w.w;
-    }
-    static __device__ __forceinline__ void store(float* p, const float (&f)[4]) {
-        *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-    }
+    typedef float4 Raw;
+    static __device__ __forceinline__ Raw load(const float* p) { return *reinterpret_cast<const float4*>(p); }
+    static __device__ __forceinline__ void split(const Raw& w, float (&f)[4]) { f[0] = w.x; f[1] = w.y; f[2] = w.z; f[3] = w.w; }
+    static __device__ __forceinline__ void store(float* p, const float (&f)[4]) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
 };
 template <typename T>
 struct Elements<T, 1> {
-    static __device__ __forceinline__ void load(const T* p, float (&f)[1]) { f[0] = (float)*p; }
+    typedef T Raw;
+    static __device__ __forceinline__ Raw load(const T* p) { return *p; }
+    static __device__ __forceinline__ void split(const Raw& w, float (&f)[1]) { f[0] = (float)w; }
     static __device__ __forceinline__ void store(T* p, const float (&f)[1]) { *p = (T)f[0]; }
 };
 
@@ -139,18 +140,38 @@ __global__ void __launch_bounds__(kNormBlock<T, VEC, TPR>) k_block_norm(const __
     const long long row = (long long)blockIdx.x * PER_BLOCK + threadIdx.x / TPR;
     if (row >= a.rows) return;                                              // (whole warps: TPR is a multiple of 32)
     const int t = threadIdx.x % TPR;
+    typename E::Raw x[NCH], residual[NCH], gate[NCH];
+    {
+        const T *const xs = (const T*)a.x + row * a.x_row, *const rs = (const T*)a.residual + row * a.residual_row, *const gs = (const T*)a.gate_rows + row * a.gate_row;
+#pragma unroll
+        for (int c = 0; c < NCH; c++) {
+            const int at = (c * TPR + t) * VEC;
+            if (at < a.dim) x[c] = E::load(xs + at);
+        }
+        if (a.residual != nullptr)
+#pragma unroll
+            for (int c = 0; c < NCH; c++) {
+                const int at = (c * TPR + t) * VEC;
+                if (at < a.dim) residual[c] = E::load(rs + at);
+            }
+        if (a.gate_rows != nullptr)
+#pragma unroll
+            for (int c = 0; c < NCH; c++) {
+                const int at = (c * TPR + t) * VEC;
+                if (at < a.dim) gate[c] = E::load(gs + at);
+            }
+    }
     float r[NCH][VEC];
-    uint32_t largest = 0;
-    const T* x = (const T*)a.x + row * a.x_row;
-    float squares = 0.0f;
 #pragma unroll
     for (int c = 0; c < NCH; c++) {
         const int at = (c * TPR + t) * VEC;
-        if (at < a.dim) E::load(x + at, r[c]);
+        if (at < a.dim) E::split(x[c], r[c]);
         else
 #pragma unroll
             for (int i = 0; i < VEC; i++) r[c][i] = 0.0f;
     }
+    uint32_t largest = 0;
+    float squares = 0.0f;
     if (a.post_norm != nullptr) {
 #pragma unroll
         for (int c = 0; c < NCH; c++)
@@ -181,12 +202,12 @@ __global__ void __launch_bounds__(kNormBlock<T, VEC, TPR>) k_block_norm(const __
             for (int i = 0; i < VEC; i++) r[c][i] *= w[i];
         }
         if (a.gate_rows != nullptr) {
-            E::load((const T*)a.gate_rows + row * a.gate_row + at, w);
+            E::split(gate[c], w);
 #pragma unroll
             for (int i = 0; i < VEC; i++) r[c][i] *= w[i];
         }
         if (a.residual != nullptr) {
-            E::load((const T*)a.residual + row * a.residual_row + at, w);
+            E::split(residual[c], w);
 #pragma unroll
             for (int i = 0; i < VEC; i++) r[c][i] = fmaf(a.residual_scale, w[i], r[c][i]);
         }
@@ -237,19 +258,31 @@ __global__ void __launch_bounds__(kNormBlock<T, VEC, TPR>) k_quantize_rows(const
     const long long row = (long long)blockIdx.x * PER_BLOCK + threadIdx.x / TPR;
     if (row >= a.rows) return;
     const int t = threadIdx.x % TPR;
+    typename E::Raw x[NCH], b[NCH];
+    const T* xs = (const T*)a.x + row * a.x_row;
+#pragma unroll
+    for (int c = 0; c < NCH; c++) {
+        const int at = (c * TPR + t) * VEC;
+        if (at < a.dim) x[c] = E::load(xs + at);
+    }
+    if (a.gated)
+#pragma unroll
+        for (int c = 0; c < NCH; c++) {
+            const int at = (c * TPR + t) * VEC;
+            if (at < a.dim) b[c] = E::load(xs + a.dim + at);
+        }
     float r[NCH][VEC];
     uint32_t largest = 0;
-    const T* x = (const T*)a.x + row * a.x_row;
 #pragma unroll
     for (int c = 0; c < NCH; c++) {
         const int at = (c * TPR + t) * VEC;
         if (at >= a.dim) continue;
-        E::load(x + at, r[c]);
+        E::split(x[c], r[c]);
         if (a.gated) {
-            float b[VEC];
-            E::load(x + a.dim + at, b);
+            float g[VEC];
+            E::split(b[c], g);
 #pragma unroll
-            for (int i = 0; i < VEC; i++) r[c][i] = r[c][i] / (1.0f + expf(-r[c][i])) * b[i];
+            for (int i = 0; i < VEC; i++) r[c][i] = r[c][i] / (1.0f + expf(-r[c][i])) * g[i];
         }
 #pragma unroll
         for (int i = 0; i < VEC; i++) largest = max(largest, __float_as_uint(r[c][i]) & 0x7fffffffu);

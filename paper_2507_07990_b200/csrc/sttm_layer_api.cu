@@ -21,23 +21,29 @@ sttm_status by_element(int dtype, F&& f) {
     return dtype == STTM_BF16 ? f(__nv_bfloat16()) : dtype == STTM_F16 ? f(__half()) : f(0.0f);
 }
 
-// Threads per row and chunks per thread: the fewest threads that hold a row in so many chunks each (four of 16 bytes, 16 single
+// Threads per row and chunks per thread: the fewest threads that hold a row in so many chunks each (four of 16 bytes, eight single
 // elements where rows do not fill whole 16-byte words).
 template <typename T, int VEC, bool QUANTIZE>
 sttm_status launch_rows(const NormArgs& a, void* stream) {
-    constexpr int NCH = VEC == 1 ? 16 : VEC == 4 ? 8 : 4;
-    auto go = [&](auto tpr) -> sttm_status {
-        constexpr int TPR = decltype(tpr)::value, BLOCK = kNormBlock<T, VEC, TPR>, PER = BLOCK / TPR;
+    constexpr int NCH = VEC == 8 ? 4 : 8;
+    auto go = [&](auto tpr, auto nch) -> sttm_status {
+        constexpr int TPR = decltype(tpr)::value, N = decltype(nch)::value, BLOCK = kNormBlock<T, VEC, TPR>, PER = BLOCK / TPR;
         const long long grid = (a.rows + PER - 1) / PER;
-        if constexpr (QUANTIZE) return launch(k_quantize_rows<T, VEC, TPR, NCH>, grid, BLOCK, 0, 0, stream, a);
-        else return launch(k_block_norm<T, VEC, TPR, NCH>, grid, BLOCK, 0, 0, stream, a);
+        if constexpr (QUANTIZE) return launch(k_quantize_rows<T, VEC, TPR, N>, grid, BLOCK, 0, 0, stream, a);
+        else return launch(k_block_norm<T, VEC, TPR, N>, grid, BLOCK, 0, 0, stream, a);
     };
+    const std::integral_constant<int, NCH> nch{};
     const int per_thread = NCH * VEC;
-    if (a.dim <= 32 * per_thread) return go(std::integral_constant<int, 32>());
-    if (a.dim <= 128 * per_thread) return go(std::integral_constant<int, 128>());
-    if (a.dim <= 256 * per_thread) return go(std::integral_constant<int, 256>());
-    if (a.dim <= 512 * per_thread) return go(std::integral_constant<int, 512>());
-    return go(std::integral_constant<int, 1024>());
+    if (a.dim <= 32 * per_thread) return go(std::integral_constant<int, 32>(), nch);
+    if (a.dim <= 128 * per_thread) return go(std::integral_constant<int, 128>(), nch);
+    if (a.dim <= 256 * per_thread) return go(std::integral_constant<int, 256>(), nch);
+    if (a.dim <= 512 * per_thread) return go(std::integral_constant<int, 512>(), nch);
+    if constexpr (VEC == 1) {
+        if (a.dim <= 1024 * per_thread) return go(std::integral_constant<int, 1024>(), nch);
+        return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 2 * NCH>());
+    } else {
+        return STTM_ERR_UNSUPPORTED;                            // (512 threads hold kNormMaxDim)
+    }
 }
 
 struct MatmulPlan {
@@ -190,7 +196,7 @@ sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream) {
     a.blocks = (p->inner + kMatK - 1) / kMatK;
     a.a_tiles = (int)pl.a_tiles; a.b_tiles = (int)pl.b_tiles;
     a.cluster = pl.cluster;
-    a.stages = pl.stages;
+    a.stages = (uint32_t)pl.stages;
     a.status = p->device_status;
     a.wide = !misaligned(p->out, 16) && (p->rows == 1 || p->out_row * e % 16 == 0);
     CUtensorMap mx, mw;

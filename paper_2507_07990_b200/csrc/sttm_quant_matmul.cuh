@@ -26,7 +26,7 @@ struct MatmulArgs {
     int blocks;                   // steps of 128 along the inner axis
     int a_tiles, b_tiles;         // tiles of 128 rows, of NT rows
     int cluster;                  // CTAs that share the inner axis (SWAP), or 1
-    int stages;
+    uint32_t stages;
     int32_t* status;
     bool wide;                    // rows of out can be written in 16-byte pieces
 };
@@ -99,6 +99,18 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // this CTA's tiles, and its part of the inner axis
+    const int size = a.cluster, rank = size > 1 ? (int)cluster_rank() : 0;
+    const int tiles = a.a_tiles * a.b_tiles, first = blockIdx.x / size, step = gridDim.x / size;
+    const int k0 = (int)((long long)a.blocks * rank / size), k1 = (int)((long long)a.blocks * (rank + 1) / size);
+    if (warp == 0) {
+        // The weights are called into L2 while the kernel before still runs (whatever that writes, L2 has it too).
+        if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &map_b : &map_a)) : "memory");
+        int ta, tb;
+        tile_at(a, first, ta, tb);
+        if (lane < min(k1 - k0, 32))
+            asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(&map_a)), "r"((k0 + lane) * kMatK), "r"(ta * 128) : "memory");
+    }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_word)), "r"(COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -110,52 +122,58 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
     wait_for_prior_kernel();
     let_next_kernel_start();
 
-    // this CTA's tiles, and its part of the inner axis
-    const int size = a.cluster, rank = size > 1 ? (int)cluster_rank() : 0;
-    const int tiles = a.a_tiles * a.b_tiles, first = blockIdx.x / size, step = gridDim.x / size;
-    const int k0 = (int)((long long)a.blocks * rank / size), k1 = (int)((long long)a.blocks * (rank + 1) / size);
     bool timed_out = false;
-    int q = 0, n = 0;                                           // slots and accumulators taken up so far
+    int n = 0;                                                  // accumulators taken up so far
 
     if (warp == 0) {
+        uint32_t slot = 0, turn = 1, taken = 0;                 // (the first wait for every slot returns at once: the phase before the first)
         for (int tile = first; tile < tiles && !timed_out; tile += step) {
             int ta, tb;
             tile_at(a, tile, ta, tb);
-            for (int k = k0; k < k1; k++, q++) {
-                const int s = q % a.stages;
-                if (q >= a.stages && !mbar_wait(empty + 8 * s, q / a.stages - 1, timed_out)) break;
+#pragma unroll 1
+            for (int k = k0; k < k1; k++) {
+                if (!mbar_wait_near(empty + 8 * slot, turn, timed_out)) break;
                 if (lane == 0) {
-                    mbar_expect_tx(full + 8 * s, SLOT);
-                    copy_tile_2d(ring + s * SLOT, &map_a, k * kMatK, ta * 128, full + 8 * s);
-                    copy_tile_2d(ring + s * SLOT + 128 * kMatK, &map_b, k * kMatK, tb * NT, full + 8 * s);
+                    mbar_expect_tx(full + 8 * slot, SLOT);
+                    copy_tile_2d(ring + slot * SLOT, &map_a, k * kMatK, ta * 128, full + 8 * slot);
+                    copy_tile_2d(ring + slot * SLOT + 128 * kMatK, &map_b, k * kMatK, tb * NT, full + 8 * slot);
                 }
                 __syncwarp();
+                taken++;
+                if (++slot == a.stages) {
+                    slot = 0;
+                    turn ^= 1;
+                }
             }
         }
         // the CTA must not end with copies in flight
-        for (int p = max(0, q - a.stages); p < q; p++) {
+        for (uint32_t p = taken > a.stages ? taken - a.stages : 0; p < taken; p++) {
             bool late = false;
-            mbar_wait_sleep(full + 8 * (p % a.stages), p / a.stages, late);
+            mbar_wait_sleep(full + 8 * (p % a.stages), (int)(p / a.stages), late);
             timed_out |= late;
         }
     } else if (warp == 1) {
+        const uint32_t ring_lo = one_value((uint32_t)tc_operand(ring)), tm = one_value(tmem), bar = one_value(bars);
+        uint32_t slot = 0, turn = 0;
         for (int tile = first; tile < tiles && !timed_out; tile += step, n++) {
-            const int b = n & 1;
-            if (n >= 2 && !mbar_wait(acc_empty + 8 * b, (n >> 1) - 1, timed_out)) break;
+            const uint32_t b = one_value(n & 1);
+            if (n >= 2 && !mbar_wait_near(acc_empty + 8 * b, (n >> 1) - 1, timed_out)) break;
             tc_fence_after();
-            for (int k = k0; k < k1; k++, q++) {
-                const int s = q % a.stages;
-                if (!mbar_wait(full + 8 * s, q / a.stages, timed_out)) break;
-                tc_fence_after();
-                if (lane == 0) {
-                    const uint64_t da = tc_operand(ring + s * SLOT), db = tc_operand(ring + s * SLOT + 128 * kMatK);
+#pragma unroll 1
+            for (int k = k0; k < k1; k++) {
+                const uint32_t at = one_value(slot), lo = ring_lo + at * (SLOT / 16), more = one_value(k > k0), last = one_value(k + 1 == k1);
+                if (!mbar_wait_near(full + 8 * slot, turn, timed_out)) break;
+                if (elected()) {
 #pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        mma_i8(tmem + b * NT, (uint32_t)da + 2 * i, (uint32_t)db + 2 * i, (uint32_t)(da >> 32), matmul_idesc(NT), k > k0 || i > 0);
-                    tc_commit(empty + 8 * s);
-                    if (k + 1 == k1) tc_commit(acc_full + 8 * b);
+                    for (int i = 0; i < 4; i++) mma_i8(tm + b * NT, lo + 2 * i, lo + 128 * kMatK / 16 + 2 * i, kOperandHigh, matmul_idesc(NT), i > 0 ? 1 : more);
+                    tc_commit(bar + 8 * kMatMaxStages + 8 * at);
+                    if (last) tc_commit(bar + 16 * kMatMaxStages + 8 * b);
                 }
                 __syncwarp();
+                if (++slot == a.stages) {
+                    slot = 0;
+                    turn ^= 1;
+                }
             }
         }
         // the last products have completed before the tensor memory is given back
