@@ -478,6 +478,7 @@ typedef struct sttm_norm_params {
     int8_t* q;                    /* [rows][dim] out, or NULL                                      */
     long long q_row;              /* bytes                                                         */
     float* q_scale;               /* [rows] out (with q)                                           */
+    int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_TIMEOUT                 */
 } sttm_norm_params;
 sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream);
 
@@ -496,6 +497,7 @@ typedef struct sttm_quantize_params {
     int8_t* q;                    /* [rows][dim] out                                               */
     long long q_row;              /* bytes                                                         */
     float* scale;                 /* [rows] out                                                    */
+    int32_t* device_status;       /* as for sttm_block_norm                                        */
 } sttm_quantize_params;
 sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream);
 

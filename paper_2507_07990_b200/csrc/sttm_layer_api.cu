@@ -21,29 +21,49 @@ sttm_status by_element(int dtype, F&& f) {
     return dtype == STTM_BF16 ? f(__nv_bfloat16()) : dtype == STTM_F16 ? f(__half()) : f(0.0f);
 }
 
-// Threads per row and chunks per thread: the fewest threads that hold a row in so many chunks each (four of 16 bytes, eight single
-// elements where rows do not fill whole 16-byte words).
+// Many rows: a warp each out of shared memory, where that holds six or more and every warp gets four or more (55724 rows of 3584 bf16, both norms and a
+// gate: 280 us against 305 in blocks; 15630 of 1157 fp16 with gates of their own 54 against 92; but 5278 rows, 2.4 a warp, 35 against 28).
+// Else a block each: short rows a warp, few rows the fewest threads that hold one with one chunk (of 16 bytes, or of one element where rows do not
+// fill whole 16-byte words) each, two of fp32, eight single elements (one row of 3584: 4.1 us on its own, with four chunks a thread 5.9); more rows
+// than the GPU takes at once four chunks a thread (5278 rows: 28 us, with one 35).
 template <typename T, int VEC, bool QUANTIZE>
 sttm_status launch_rows(const NormArgs& a, void* stream) {
-    constexpr int NCH = VEC == 8 ? 4 : 8;
+    RowsShape shape;
+    const int arrays = a.gate_rows != nullptr ? 3 : 2, weights = (a.post_norm != nullptr) + (a.gate != nullptr) + (a.pre_norm != nullptr);
+    shape.pitch = (uint32_t)align_up((size_t)a.dim * sizeof(T) + (VEC == 1 ? 32 : 0), 128);
+    shape.weights = (uint32_t)align_up((size_t)a.dim * 4, 128);
+    const int fit = ((int)kRowsSmem - 1024 - weights * (int)shape.weights) / (int)(arrays * shape.pitch + 8);
+    shape.warps = std::max(1, std::min(fit, kRowsWarps));
+    shape.slots = std::min(4, fit / shape.warps);
+    if (fit >= 6 && a.dim >= 64 && a.rows >= 4ll * shape.warps * shape.slots * sm_count()) {
+        static size_t allowed[kMaxDevices] = {};
+        const sttm_status s = allow_smem((const void*)k_norm_rows<T, VEC, QUANTIZE>, kRowsSmem, allowed);
+        if (s != STTM_OK) return s;
+        const size_t smem = (size_t)shape.warps * shape.slots * arrays * shape.pitch + align_up((size_t)shape.warps * shape.slots * 8, 128) + weights * shape.weights;
+        const long long grid = std::min<long long>((a.rows + shape.warps - 1) / shape.warps, sm_count());
+        return launch(k_norm_rows<T, VEC, QUANTIZE>, grid, shape.warps * 32, smem, 0, stream, a, shape);
+    }
     auto go = [&](auto tpr, auto nch) -> sttm_status {
-        constexpr int TPR = decltype(tpr)::value, N = decltype(nch)::value, BLOCK = kNormBlock<T, VEC, TPR>, PER = BLOCK / TPR;
+        constexpr int TPR = decltype(tpr)::value, N = decltype(nch)::value, BLOCK = norm_block(TPR), PER = BLOCK / TPR;
         const long long grid = (a.rows + PER - 1) / PER;
         if constexpr (QUANTIZE) return launch(k_quantize_rows<T, VEC, TPR, N>, grid, BLOCK, 0, 0, stream, a);
         else return launch(k_block_norm<T, VEC, TPR, N>, grid, BLOCK, 0, 0, stream, a);
     };
+    constexpr int NCH = VEC == 1 ? 8 : VEC == 4 ? 2 : 1;
     const std::integral_constant<int, NCH> nch{};
     const int per_thread = NCH * VEC;
+    if constexpr (VEC > 1) {
+        const std::integral_constant<int, 32 / VEC> four{};
+        if (a.dim <= 1024) return go(std::integral_constant<int, 32>(), four);
+        if (a.rows > 2ll * sm_count() && a.dim <= 4096) return go(std::integral_constant<int, 128>(), four);
+        if (a.rows > 2ll * sm_count() && a.dim <= 8192) return go(std::integral_constant<int, 256>(), four);
+    }
     if (a.dim <= 32 * per_thread) return go(std::integral_constant<int, 32>(), nch);
     if (a.dim <= 128 * per_thread) return go(std::integral_constant<int, 128>(), nch);
     if (a.dim <= 256 * per_thread) return go(std::integral_constant<int, 256>(), nch);
     if (a.dim <= 512 * per_thread) return go(std::integral_constant<int, 512>(), nch);
-    if constexpr (VEC == 1) {
-        if (a.dim <= 1024 * per_thread) return go(std::integral_constant<int, 1024>(), nch);
-        return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 2 * NCH>());
-    } else {
-        return STTM_ERR_UNSUPPORTED;                            // (512 threads hold kNormMaxDim)
-    }
+    if (a.dim <= 1024 * per_thread) return go(std::integral_constant<int, 1024>(), nch);
+    return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 2 * NCH>());
 }
 
 struct MatmulPlan {
@@ -126,7 +146,7 @@ sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream) {
         wide = wide && (in[i] == nullptr || (!misaligned(in[i], 16) && (p->rows == 1 || in_row[i] * e % 16 == 0)));
         wide = wide && (out[i] == nullptr || i == 2 || (!misaligned(out[i], 16) && (p->rows == 1 || out_row[i] * e % 16 == 0)));
     }
-    if (odd_address(p->post_norm, p->gate, p->pre_norm, p->q_scale)) return STTM_ERR_ARG;
+    if (odd_address(p->post_norm, p->gate, p->pre_norm, p->q_scale, p->device_status)) return STTM_ERR_ARG;
     const uintptr_t weights = (uintptr_t)p->post_norm | (uintptr_t)p->gate | (uintptr_t)p->pre_norm;
     wide = wide && weights % 16 == 0 && (p->q == nullptr || (!misaligned(p->q, 8) && (p->rows == 1 || p->q_row % 8 == 0)));
     for (int o = 0; o < 3; o++) {
@@ -146,6 +166,7 @@ sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream) {
     a.sum = p->sum; a.out = p->out;
     a.sum_row = p->sum_row; a.out_row = p->out_row;
     a.q = p->q; a.q_row = p->q_row; a.q_scale = p->q_scale;
+    a.status = p->device_status;
     a.rows = p->rows;
     a.dim = p->dim;
     return by_element(p->dtype, [&](auto tag) {
@@ -158,7 +179,7 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream) {
     if (p == nullptr || p->rows < 0 || p->dim < 1 || !known_type(p->dtype)) return STTM_ERR_ARG;
     if (p->dim > kNormMaxDim || p->rows > INT_MAX) return STTM_ERR_UNSUPPORTED;
     if (p->rows == 0) return STTM_OK;
-    if (p->x == nullptr || p->q == nullptr || p->scale == nullptr || odd_address(p->scale)) return STTM_ERR_ARG;
+    if (p->x == nullptr || p->q == nullptr || p->scale == nullptr || odd_address(p->scale, p->device_status)) return STTM_ERR_ARG;
     const long long e = p->dtype == STTM_F32 ? 4 : 2, in = p->gated ? 2ll * p->dim : p->dim;
     if (misaligned(p->x, e) || (p->rows > 1 && (p->x_row < in || p->q_row < p->dim || p->x_row > LLONG_MAX / 4 / p->rows || p->q_row > LLONG_MAX / 4 / p->rows)))
         return STTM_ERR_ARG;
@@ -167,6 +188,7 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream) {
     NormArgs a = {};
     a.x = p->x; a.x_row = p->x_row;
     a.q = p->q; a.q_row = p->q_row; a.q_scale = p->scale;
+    a.status = p->device_status;
     a.rows = p->rows;
     a.dim = p->dim;
     a.gated = p->gated != 0;

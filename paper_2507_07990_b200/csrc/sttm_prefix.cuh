@@ -267,29 +267,6 @@ __device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
     for (int i = 0; i < 32; i += 8)
         asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]));
 }
-// two numbers at a time
-__device__ __forceinline__ uint64_t both(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void apart(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-// the largest of three; NaN if one is
-__device__ __forceinline__ float max3(float x, float y, float z) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
-    return r;
-}
 // 2^x twice without the special-function unit, for x in [-126, 127) (below: 2^-126): x = n + f with |f| <= 1/2, 2^f by the polynomial
 // of degree 4 whose largest relative error is least (2.6e-6: Remez exchange over [-1/2, 1/2]), n added to the exponent.
 __device__ __forceinline__ void exp2_pair(uint64_t x, float& x0, float& x1) {

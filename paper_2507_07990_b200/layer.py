@@ -3,8 +3,8 @@ matrix products of them.
 
 ``NormPlan`` (sttm_block_norm), ``QuantizePlan`` (sttm_quantize_rows) and ``MatmulPlan`` (sttm_quant_matmul)
 marshal arguments; a plan holds buffers for up to ``max_rows`` rows and what does not change from call to call.  The functions
-of the C names are single calls.  All work is enqueued on the current stream, nothing synchronises.  A plan's outputs are its own
-buffers unless the call is given others: they stand until its next call, so use a plan on one stream, or order the
+of the C names are single calls.  All work is enqueued on the current stream, nothing synchronises; conditions found on the device are
+OR-ed into a plan's ``status``, which it never clears.  A plan's outputs are its own buffers unless the call is given others: they stand until its next call, so use a plan on one stream, or order the
 streams.  There is no fallback.
 """
 from __future__ import annotations
@@ -27,12 +27,12 @@ class NormParams(C.Structure):
                 ("residual_row", C.c_longlong), ("gate_row", C.c_longlong), ("rows", C.c_longlong), ("dim", C.c_int), ("dtype", C.c_int),
                 ("post_norm", C.c_void_p), ("gate", C.c_void_p), ("pre_norm", C.c_void_p), ("residual_scale", C.c_float), ("eps", C.c_float),
                 ("sum", C.c_void_p), ("out", C.c_void_p), ("sum_row", C.c_longlong), ("out_row", C.c_longlong),
-                ("q", C.c_void_p), ("q_row", C.c_longlong), ("q_scale", C.c_void_p)]
+                ("q", C.c_void_p), ("q_row", C.c_longlong), ("q_scale", C.c_void_p), ("device_status", C.c_void_p)]
 
 
 class QuantizeParams(C.Structure):
     _fields_ = [("x", C.c_void_p), ("x_row", C.c_longlong), ("rows", C.c_longlong), ("dim", C.c_int), ("dtype", C.c_int), ("gated", C.c_int),
-                ("q", C.c_void_p), ("q_row", C.c_longlong), ("scale", C.c_void_p)]
+                ("q", C.c_void_p), ("q_row", C.c_longlong), ("scale", C.c_void_p), ("device_status", C.c_void_p)]
 
 
 class MatmulParams(C.Structure):
@@ -107,7 +107,9 @@ class NormPlan:
         self.sum = torch.empty((max_rows, dim), dtype=dtype, device=device)
         self.out = torch.empty((max_rows, dim), dtype=dtype, device=device) if self.normed else None
         self.rows = empty_quant_rows(max_rows, dim, device) if quantize else None
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
         p = self.params = NormParams()
+        p.device_status = self.status.data_ptr()
         p.dim, p.dtype, p.residual_scale, p.eps = dim, _TYPES[dtype], residual_scale, eps
         p.post_norm, p.gate, p.pre_norm = (_weights(t, dim, self.index, n) for t, n in ((post_norm, "post_norm"), (gate, "gate"), (pre_norm, "pre_norm")))
         self.at, self.call = C.byref(p), binding.load_library().sttm_block_norm
@@ -149,7 +151,9 @@ class QuantizePlan:
         _want(dtype in _TYPES and dim >= 1 and max_rows >= 0, "rows must be bf16, fp16 or fp32, of at least one channel")
         self.index, self.width, self.dtype, self.max_rows = _index(device), 2 * dim if gated else dim, dtype, max_rows
         self.rows = empty_quant_rows(max_rows, dim, torch.device("cuda", self.index))
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.rows.q.device)
         p = self.params = QuantizeParams()
+        p.device_status = self.status.data_ptr()
         p.dim, p.dtype, p.gated = dim, _TYPES[dtype], int(gated)
         p.q, p.q_row, p.scale = self.rows.q.data_ptr(), self.rows.q.stride(0), self.rows.scale.data_ptr()
         self.at, self.call = C.byref(p), binding.load_library().sttm_quantize_rows

@@ -89,6 +89,37 @@ def test_block_norm_strides_and_in_place(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width,stride,shift", [(3584, 3584, 0), (1157, 1157, 0), (96, 104, 8), (67, 67, 3), (1000, 1003, 1), (2048, 2056, 0)])
+def test_many_rows(dtype, width, stride, shift):
+    # a warp to a row, out of shared memory; rows that share 16-byte words with their neighbours, in place too
+    gen = torch.Generator().manual_seed(width)
+    rows = 1301
+    w = [(1 + 0.3 * torch.randn(width, generator=gen)).cuda() for _ in range(3)]
+    x, residual, gate = (rows_of(gen, rows, width, dtype, stride, shift) for _ in range(3))
+    for kw, g in [(dict(post_norm=w[0], gate=w[1], pre_norm=w[2], residual_scale=0.7), None), (dict(pre_norm=w[2]), gate),
+                  (dict(post_norm=w[0], pre_norm=w[2], quantize=True), gate)]:
+        plan = layer.NormPlan(width, dtype, rows, eps=1e-5, **kw)
+        got = plan.run(x, residual, gate=g)
+        gates = [t for t in (kw.get("gate"), g) if t is not None]
+        check_norm(got, x, residual, kw.get("post_norm"), gates, kw.get("residual_scale", 1.0), w[2], 1e-5, kw.get("quantize"))
+        want, mine = got.sum.clone(), residual.clone()
+        room = rows_of(gen, rows, width, dtype, stride, shift)
+        room.copy_(mine)
+        assert torch.equal(plan.run(x, room, gate=g, sum=room).sum, want) and int(plan.status) == 0
+    got = layer.NormPlan(width, dtype, rows, pre_norm=w[2], eps=1e-5).run(x)
+    check_norm(got, x, None, None, [], 1.0, w[2], 1e-5, False)
+    for gated in (False, True):
+        z = rows_of(gen, rows, 2 * width, dtype, 2 * stride, shift) if gated else x
+        y = z.double()
+        if gated:
+            y = y[:, :width] * torch.sigmoid(y[:, :width]) * y[:, width:]
+        q = layer.sttm_quantize_rows(z, gated)
+        step = y.abs().amax(1, keepdim=True) / 127
+        assert not ((q.scale.double() - step[:, 0]).abs() > 2.0 ** -18 * step[:, 0]).any()
+        assert not ((q.dequantized().double() - y).abs() > step * (0.5 + 127 * 2.0 ** -17)).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,width", [(1, 14336), (33, 64), (5, 1157), (4, 3584), (3, 1), (2, 16384)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_quantize_rows(dtype, rows, width, gated):
