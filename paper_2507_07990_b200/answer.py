@@ -6,19 +6,20 @@ together, as a video LLM would.
 ``Answerer.watch`` merges a video and fills one cache per layer with its rows, rotated by the rows' position
 ids.  ``Answerer.ask`` puts several questions to it at once: they share the video's full pages; their tokens go
 through the layers one by one, collecting the attention that every slot receives; the video's rows that no
-question token looks at are evicted; the answers are read from what is left.  Weights are random: this shows
-the path, not a model.  Projections are plain matrix products, and the video's own layers (a prefill) use torch's
-attention; norms of queries and keys, rotation, cache entry, cached attention and eviction are the library's.
+question token looks at are evicted; the answers are read from what is left.  ``Answerer.ask_together`` reads whole questions,
+of any lengths, in one go and keeps nothing of the video but the one cache that they share.  Weights are random: this shows
+the path, not a model.  Projections are plain matrix products, or with ``Config.int8`` the library's in 8 bits, and the video's own layers
+(a prefill) use torch's attention; norms, rotation, cache entry, cached attention and eviction are the library's.
 """
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import Iterable, List, Optional
+from typing import Iterable, List, Optional, Sequence
 
 import torch
 import torch.nn.functional as F
 
-from . import binding, cache
+from . import binding, cache, layer as decoder, prefix
 
 
 @dataclass
@@ -33,6 +34,7 @@ class Config:
     page: int = 16
     theta: float = 1e6
     dtype: torch.dtype = torch.bfloat16
+    int8: bool = False           # the layers' projections in 8 bits
 
 
 def _rms(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
@@ -58,20 +60,34 @@ class Answerer:
         self.layers = [dict(norm1=one(c.width), qkv=mat(c.width, heads * c.dim), q_norm=one(c.dim), k_norm=one(c.dim),
                             out=mat(c.q_heads * c.dim, c.width), norm2=one(c.width), up=mat(c.width, 2 * c.hidden), down=mat(c.hidden, c.width))
                        for _ in range(c.layers)]
+        if c.int8:                                               # every projection's output channels
+            for layer in self.layers:
+                layer["rows"] = {name: decoder.sttm_quantize_rows(layer[name].t().contiguous()) for name in ("qkv", "out", "up", "down")}
         self.norm, self.embed, self.head = one(c.width), mat(c.vocab, c.width) * c.vocab ** 0.5, mat(c.width, c.vocab)
         self.pools: List[cache.PagedCache] = []                  # one per layer, once a video has been watched
         half = c.dim // 2
         self.rotary = cache.Rotary((c.theta ** (-torch.arange(half, dtype=torch.float64) / half)).float().to(device))
 
-    def _qkv(self, layer: dict, x: torch.Tensor):
+    def _project(self, layer: dict, name: str, x: torch.Tensor, gated: bool = False) -> torch.Tensor:
+        """``x`` (gated: ``silu(a) * b`` of rows ``[a | b]``) times one of a layer's weights."""
+        if self.cfg.int8:
+            return decoder.sttm_quant_matmul(decoder.sttm_quantize_rows(x, gated), layer["rows"][name], self.cfg.dtype)
+        if gated:
+            gate, up = x.chunk(2, -1)
+            x = F.silu(gate) * up
+        return x @ layer[name]
+
+    def _heads(self, y: torch.Tensor):
         c = self.cfg
-        y = (_rms(x, layer["norm1"]) @ layer["qkv"]).view(-1, c.q_heads + 2 * c.kv_heads, c.dim)
+        y = y.view(-1, c.q_heads + 2 * c.kv_heads, c.dim)
         return y[:, :c.q_heads], y[:, c.q_heads:c.q_heads + c.kv_heads], y[:, c.q_heads + c.kv_heads:]
 
+    def _qkv(self, layer: dict, x: torch.Tensor):
+        return self._heads(self._project(layer, "qkv", _rms(x, layer["norm1"])))
+
     def _rest(self, layer: dict, x: torch.Tensor, attended: torch.Tensor) -> torch.Tensor:
-        x = x + attended.reshape(x.shape[0], -1) @ layer["out"]
-        gate, up = (_rms(x, layer["norm2"]) @ layer["up"]).chunk(2, -1)
-        return x + (F.silu(gate) * up) @ layer["down"]
+        x = x + self._project(layer, "out", attended.reshape(x.shape[0], -1))
+        return x + self._project(layer, "down", self._project(layer, "up", _rms(x, layer["norm2"])), gated=True)
 
     def _append_plan(self, pool: cache.PagedCache, layer: dict) -> cache.AppendPlan:
         return cache.AppendPlan(pool, self.cfg.q_heads, self.rotary, q_norm=layer["q_norm"], k_norm=layer["k_norm"])
@@ -140,6 +156,34 @@ class Answerer:
                     attend=[cache.AttendPlan(p, self.cfg.q_heads) for p in pools],
                     scores=[torch.zeros((questions, p.heads, slots), device=self.device) for p in pools] if scored else None)
 
+    def ask_together(self, questions: Sequence[torch.Tensor], answer_tokens: int) -> torch.Tensor:
+        """``questions``: token ids, one tensor a question, of any lengths.  Every question sees the video's cache, which is read once for all
+        of them, and its own tokens; the questions are read in one go.  Returns greedy answers ``[questions, answer_tokens]``."""
+        lengths = [int(q.numel()) for q in questions]
+        if not lengths or min(lengths) < 1 or any(q.dim() != 1 for q in questions) or answer_tokens < 1:
+            raise ValueError("questions must be one-dimensional, of at least one token each, answer_tokens at least 1")
+        if not self.pools:
+            raise ValueError("no video has been watched")
+        c, n = self.cfg, len(lengths)
+        own = [cache.empty_cache(n, max(lengths) + answer_tokens, c.kv_heads, c.dim, c.page, c.dtype, self.device) for _ in self.pools]
+        state = Together(self, own, sum(lengths))
+        ends = torch.tensor(lengths, device=self.device).cumsum(0)
+        offsets = torch.cat([ends.new_zeros(1), ends])
+        positions = torch.cat([self.next_position + torch.arange(m, device=self.device, dtype=torch.int32) for m in lengths])
+        last = state.step(torch.cat(list(questions)), offsets, positions)[ends - 1]
+        offsets, positions = torch.arange(n + 1, device=self.device), positions[ends - 1]
+        answers = []
+        for _ in range(answer_tokens):
+            logits = (last @ self.head).float()
+            tokens = logits.argmax(-1)
+            answers.append(tokens)
+            if len(answers) < answer_tokens:
+                positions = positions + 1
+                last = state.step(tokens, offsets, positions)
+        self.logits = logits
+        _check_status("Answerer.ask_together", state.statuses())
+        return torch.stack(answers, 1)
+
     @staticmethod
     def _statuses(state: dict) -> List[torch.Tensor]:
         return [plan.status for plan in state["append"] + state["attend"]]
@@ -183,6 +227,49 @@ class Answerer:
         return torch.stack(answers, 1)
 
 
+class Together:
+    """Several questions through the layers at once: plans of the library's calls for up to ``max_rows`` new tokens a step."""
+
+    def __init__(self, model: Answerer, own: List[cache.PagedCache], max_rows: int):
+        c = model.cfg
+        self.model, self.lengths, self.seen = model, None, torch.tensor([model.rows], dtype=torch.int32, device=model.device)
+        self.append = [model._append_plan(pool, layer) for pool, layer in zip(own, model.layers)]
+        self.attend = [prefix.PrefixPlan(video, c.q_heads, mine, max_rows, max_prefix=model.rows) for video, mine in zip(model.pools, own)]
+        # before a layer's attention and its products, and before the head, which is not in 8 bits
+        norm = lambda w, int8: decoder.NormPlan(c.width, c.dtype, max_rows, pre_norm=w, eps=1e-6, quantize=int8, device=model.device)  # noqa: E731
+        self.norms = [norm(layer[n], c.int8) for layer in model.layers for n in ("norm1", "norm2")] + [norm(model.norm, False)]
+        self.rows, self.products = [], []
+        if c.int8:
+            quantize = lambda dim, gated: decoder.QuantizePlan(dim, c.dtype, max_rows, gated, model.device)  # noqa: E731
+            self.rows = [(quantize(c.q_heads * c.dim, False), quantize(c.hidden, True)) for _ in model.layers]
+            self.products = [{n: decoder.MatmulPlan(layer["rows"][n], c.dtype, max_rows) for n in layer["rows"]} for layer in model.layers]
+
+    def statuses(self) -> List[torch.Tensor]:
+        plans = self.append + self.attend + self.norms + [p for pair in self.rows for p in pair] + [p for layer in self.products for p in layer.values()]
+        return [p.status for p in plans]
+
+    def _project(self, i: int, name: str, x, gated: bool = False) -> torch.Tensor:
+        """``x``: rows, or for what a norm leaves its output."""
+        normed = isinstance(x, decoder.NormOutput)
+        if not self.model.cfg.int8:
+            return self.model._project(self.model.layers[i], name, x.out if normed else x, gated)
+        return self.products[i][name].run(x.rows if normed else self.rows[i][1 if gated else 0].run(x))
+
+    def step(self, tokens: torch.Tensor, offsets: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
+        """New tokens of all questions (question b's are ``offsets[b]`` ... ``offsets[b + 1] - 1``) through all layers; what comes before the head."""
+        model, lengths = self.model, self.lengths
+        stream = self.norms[0].run(model.embed[tokens])
+        for i in range(len(model.layers)):
+            q, k, v = model._heads(self._project(i, "qkv", stream))
+            entered = self.append[i].run(q, k, v, offsets, lengths, positions)
+            attended = self.attend[i].run(entered.q, offsets, self.seen, entered.new_lengths)
+            out = self._project(i, "out", attended.out.reshape(len(tokens), -1))
+            stream = self.norms[2 * i + 1].run(out, stream.sum)
+            stream = self.norms[2 * i + 2].run(self._project(i, "down", self._project(i, "up", stream), gated=True), stream.sum)
+            self.lengths = entered.new_lengths
+        return stream.out
+
+
 def main() -> None:
     from . import inputs
     cfg = Config()
@@ -196,6 +283,13 @@ def main() -> None:
     thin = model.ask(questions, 8, keep=rows // 2)
     print("%d tokens -> %d rows in the cache; answers from all of them %s, from half of them %s"
           % (spec.tokens, rows, whole.tolist(), thin.tolist()))
+    lines = [q[:12 - 3 * i] for i, q in enumerate(questions)]
+    together = model.ask_together(lines, 8)
+    cfg.int8 = True
+    model = Answerer(cfg)
+    model.watch(video, 0.97, 0.9)
+    print("questions of %s tokens read at once: answers %s, with projections in 8 bits %s"
+          % ([len(q) for q in lines], together.tolist(), model.ask_together(lines, 8).tolist()))
 
 
 if __name__ == "__main__":
