@@ -72,28 +72,63 @@ struct MatmulPlan {
     long long a_tiles, b_tiles, grid;
 };
 
+// Clusters of `size` CTAs, two to an SM, that the GPU holds at once: fewer than its SMs allow (33 of 8, 71 of 4 on 148 SMs), since a cluster lies in
+// one group of SMs.
+int matmul_clusters(int size) {
+    static int cached[kMaxDevices][9] = {};
+    const int dev = device_slot();
+    if (dev < 0) return sm_count() * 2 / size;
+    int& n = cached[dev][size];
+    if (n == 0) {
+        const auto kernel = k_quant_matmul<__nv_bfloat16, 16>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)size);
+        cfg.blockDim = dim3(kMatThreads);
+        cfg.dynamicSmemBytes = kMatSmem;
+        cudaLaunchAttribute at;
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = (unsigned)size;
+        at.val.clusterDim.y = at.val.clusterDim.z = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        static size_t allowed[kMaxDevices] = {};
+        if (allow_smem((const void*)kernel, kMatSmem, allowed) != STTM_OK || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1)
+            n = sm_count() * 2 / size;
+    }
+    return n;
+}
+
+// Few tokens take 16, 32 or 64 columns beside 128 weights.  More than 64 do so too (several tiles of 64) while two CTAs or more can share a tile's inner axis;
+// beyond, the kernel for pairs.  us, products alone, weights out of HBM, few tokens' kernel / pairs':
+//   inner x outer     tokens 64      128       256       300       400
+//   3584 x 4608      8.7 / 17.5  11.1 / 18  13.3 / 18  16.4 / 17.5 17.5 / 17.2
+//   14336 x 3584    13.9 / 41    18.7 / 41  27.5 / 41  29.0 / 41   46.2 / 40
+//   3584 x 28672    27.8 / 30    30.9 / 32
+//   1024 x 1024      5.0 / 8.0    5.0 / 8.7  5.6 / 8.7  5.8 / 8.8   6.1 / 8.8
+// A cluster shares the inner axis as widely as all clusters are resident at once (36 tiles in clusters of 8, of which 33 fit: 10.6 us, of 4: 6.7) and leaves every
+// CTA two steps.
 MatmulPlan plan_matmul(const sttm_matmul_params* p) {
     MatmulPlan pl;
     const int blocks = (p->inner + kMatK - 1) / kMatK, sms = sm_count();
-    pl.swap = p->rows <= 256;
-    pl.nt = 256;
-    if (pl.swap)
-        for (pl.nt = 16; pl.nt < p->rows;) pl.nt *= 2;
-    pl.a_tiles = pl.swap ? (p->outer + 127) / 128 : (p->rows + 255) / 256;
-    pl.b_tiles = pl.swap ? (p->rows + pl.nt - 1) / pl.nt : ((long long)p->outer + 255) / 256;
-    const long long tiles = pl.a_tiles * pl.b_tiles;
+    pl.nt = p->rows <= 16 ? 16 : p->rows <= 32 ? 32 : 64;
+    pl.a_tiles = ((long long)p->outer + 127) / 128;
+    pl.b_tiles = (p->rows + pl.nt - 1) / pl.nt;
+    long long tiles = pl.a_tiles * pl.b_tiles;
+    pl.swap = p->rows <= 64 || tiles <= sms;
     if (!pl.swap) {
+        pl.a_tiles = (p->rows + 255) / 256;
+        pl.b_tiles = ((long long)p->outer + 255) / 256;
+        tiles = pl.a_tiles * pl.b_tiles;
+        pl.nt = 256;
         pl.cluster = 2;
         pl.stages = kPairStages;
         pl.grid = 2 * std::min<long long>(tiles, sms / 2);
         return pl;
     }
-    // two CTAs to an SM where their rings and accumulators fit
-    const int per_sm = pl.nt <= 64 ? 2 : 1;
-    pl.stages = std::min(kMatMaxStages, (int)((227 * 1024 / per_sm - 1024 - matmul_fixed_bytes()) / matmul_slot(pl.nt)));
+    pl.stages = std::min(kMatMaxStages, (int)((kMatSmem - matmul_fixed_bytes()) / matmul_slot(pl.nt)));
     pl.cluster = 1;
-    while (pl.cluster < 8 && tiles * pl.cluster * 2 <= (long long)sms * per_sm && blocks >= 4 * pl.cluster) pl.cluster *= 2;
-    pl.grid = pl.cluster > 1 ? tiles * pl.cluster : std::min<long long>(tiles, (long long)sms * per_sm);
+    while (pl.cluster < 8 && blocks >= 4 * pl.cluster && tiles <= matmul_clusters(2 * pl.cluster)) pl.cluster *= 2;
+    pl.grid = pl.cluster > 1 ? tiles * pl.cluster : std::min<long long>(tiles, 2ll * sms);
     return pl;
 }
 
@@ -235,9 +270,7 @@ sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream) {
         switch (pl.nt) {
             case 16: return launch_matmul<T, 16>(a, pl, mw, mx, stream);
             case 32: return launch_matmul<T, 32>(a, pl, mw, mx, stream);
-            case 64: return launch_matmul<T, 64>(a, pl, mw, mx, stream);
-            case 128: return launch_matmul<T, 128>(a, pl, mw, mx, stream);
-            default: return launch_matmul<T, 256>(a, pl, mw, mx, stream);
+            default: return launch_matmul<T, 64>(a, pl, mw, mx, stream);
         }
     });
 }

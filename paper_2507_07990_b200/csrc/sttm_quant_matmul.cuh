@@ -33,6 +33,7 @@ struct MatmulArgs {
 
 constexpr int kMatK = 128;                            // inner elements (bytes) per step
 constexpr int kMatThreads = 6 * 32;                   // producer, products, four warps that read out
+constexpr size_t kMatSmem = 112 * 1024;               // two CTAs to an SM
 constexpr int kMatMaxStages = 8, kMatGroup = 12;      // tiles of tokens in a row before the next tile of channels (see tile_at)
 
 __host__ __device__ constexpr int matmul_slot(int nt) { return (128 + nt) * kMatK; }
@@ -58,9 +59,9 @@ __device__ __forceinline__ void copy_tile_2d(uint32_t dst, const CUtensorMap* ma
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
-__device__ __forceinline__ int ld_remote_s32(uint32_t cluster_addr) {
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
+__device__ __forceinline__ int4 ld_remote_s32x4(uint32_t cluster_addr) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(cluster_addr));
     return v;
 }
 
@@ -215,11 +216,30 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
                 if (size > 1) {                                 // (one tile per cluster then, and the ring has been read)
                     cluster_arrive();
                     cluster_wait();
-                    const int last = (int)min((long long)NT, a.rows - (long long)tb * NT);
-                    for (int col = rank; col < last; col += size) {
-                        int sum = 0;
-                        for (int r = 0; r < size; r++) sum += ld_remote_s32(map_to_rank(ring + (col * 128 + row) * 4, r));
-                        write(col, sum);
+                    // every size-th token, a warp each, four channels a lane
+                    const int last = (int)min((long long)NT, a.rows - (long long)tb * NT), ch0 = ta * 128 + 4 * lane;
+                    float scale[4], add[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        scale[i] = ch0 + i < a.outer ? a.w_scale[ch0 + i] : 0.0f;
+                        add[i] = a.bias != nullptr && ch0 + i < a.outer ? a.bias[ch0 + i] : 0.0f;
+                    }
+                    for (int col = rank + size * (warp & 3); col < last; col += 4 * size) {
+                        const uint32_t at = ring + col * 512 + lane * 16;
+                        int4 part[8];
+#pragma unroll
+                        for (int r = 0; r < 8; r++) part[r] = r < size ? ld_remote_s32x4(map_to_rank(at, r)) : make_int4(0, 0, 0, 0);
+                        int sum[4] = {0, 0, 0, 0};
+#pragma unroll
+                        for (int r = 0; r < 8; r++) {
+                            sum[0] += part[r].x; sum[1] += part[r].y; sum[2] += part[r].z; sum[3] += part[r].w;
+                        }
+                        const long long token = (long long)tb * NT + col;
+                        const float xs = a.x_scale[token];
+                        T* const out = (T*)a.out + token * a.out_row + ch0;
+#pragma unroll
+                        for (int i = 0; i < 4; i++)
+                            if (ch0 + i < a.outer) out[i] = narrow<T>((float)sum[i] * xs * scale[i] + add[i]);
                     }
                 }
             }
