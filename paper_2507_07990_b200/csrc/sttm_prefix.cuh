@@ -20,6 +20,8 @@
 // memory, and k_prefix_join puts a row's pieces together.
 #pragma once
 
+#include <climits>
+
 #include "sttm_cache.cuh"
 
 namespace sttm {
@@ -448,17 +450,17 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             const int32_t* table = c.table + (own ? walk.at - a.prefix.seqs : walk.at) * c.table_stride;
             const int at = lane * kCopyWarps + part, in_tile = at / HALVES * box, half = at % HALVES;
             const bool copies = in_tile < SLOTS;
-            // Page (`pages`, beyond the pool: zeros) and place in it of this lane's box, by the tile's number modulo four; looked up two
-            // tiles ahead.
+            // Page and place in it of this lane's box, by the tile's number modulo four; looked up two tiles ahead.  (-1: the box lies
+            // behind the last slot.  It is not copied: logits there are masked, values cleared.  `pages`, beyond the pool: zeros.)
             int page[4], place[4];
             const int slot0 = walk.u0 * SLOTS + in_tile, by_pages = SLOTS / page_slots, by_slots = SLOTS % page_slots;
             int left = walk.e.len - slot0, stretch = slot0 / page_slots, spot = slot0 - stretch * page_slots;     // of the tile looked up next
             auto look_up = [&](int& pg, int& pl) {
-                pg = pages;
+                pg = -1;
                 pl = spot;
                 if (copies && left > 0) {
                     pg = table[stretch];
-                    if (pg == pages) pg = -1;
+                    if (pg < 0) pg = INT_MAX;
                 }
                 left -= SLOTS;
                 stretch += by_pages;
@@ -469,14 +471,14 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 }
             };
             const uint32_t to = ring + half * (SLOTS * 128) + in_tile * 128;
-            const uint32_t bytes = ((SLOTS / box * HALVES + kCopyWarps - 1 - part) / kCopyWarps) * box * 128;      // this warp's of a tile
             auto copy = [&](const CUtensorMap* map, int pg, int pl) -> bool {
                 const int s = n % RING;
                 if (n >= RING && !mbar_wait_near(empty + 8 * s, n / RING - 1, timed_out)) return false;
-                if (lane == 0) mbar_expect_tx(full + 8 * s, bytes);
+                const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, pg >= 0));
+                if (lane == 0) mbar_expect_tx(full + 8 * s, boxes * box * 128);
                 __syncwarp();
-                if (copies) {
-                    if (pg < 0 || pg > pages) {
+                if (pg >= 0) {
+                    if (pg >= pages) {
                         raise_status(a.status, kStatusArg);
                         pg = pages;
                     }
@@ -828,7 +830,6 @@ constexpr int kJoinParts = 320;                                 // pieces of a r
 template <typename T, int DIM, int ROWS>
 __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid_constant__ PrefixArgs a) {
     constexpr int LANES = kPrefixJoinThreads / ROWS;            // per row
-    constexpr int AHEAD = ROWS == 8 ? 16 : 8;
     struct Row {
         const float4* from[2];    // the row's first four channels in its first piece
         int parts[2], rows[2];    // pieces; rows of the block that they lie in
@@ -901,32 +902,46 @@ __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid
     const int n = r.parts[0] + r.parts[1];
     const uint32_t token = (row0 + k) / (uint32_t)a.group;
     uint16_t* const out = a.out + ((long long)token * a.q_heads + kv * a.group + (row0 + k - token * a.group)) * DIM;
+    // CHUNKS chunks of four channels of AHEAD pieces are on their way at a time
+    constexpr int CHUNKS = DIM / 4 > LANES ? (DIM / 4 / LANES < 4 ? DIM / 4 / LANES : 4) : 1, AHEAD = 16 / CHUNKS;
 #pragma unroll 1
-    for (int chunk = threadIdx.x / ROWS; chunk < DIM / 4; chunk += LANES) {
+    for (int chunk = threadIdx.x / ROWS; chunk < DIM / 4; chunk += LANES * CHUNKS) {
         const float4 *const from0 = r.from[0] + (long long)chunk * r.rows[0], *const from1 = r.from[1] + (long long)chunk * r.rows[1];
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float4 acc[CHUNKS];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
         for (int i0 = 0; i0 < n; i0 += AHEAD) {
-            float4 o[AHEAD];
+            float4 o[AHEAD][CHUNKS];
             float f[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; u++) {
                 const int i = i0 + u;
                 f[u] = i < n ? weights[k][i] : 0.0f;
-                o[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                const bool own = i >= r.parts[0];
                 // (a piece without tiles has the weight 0: it stored no O)
-                if (f[u] != 0.0f)
-                    o[u] = i < r.parts[0] ? from0[(long long)i * (PrefixShape<DIM>::STORE * (DIM / 4))] : from1[(long long)(i - r.parts[0]) * (PrefixShape<DIM>::STORE * (DIM / 4))];
+                const float4* const from = f[u] == 0.0f ? reinterpret_cast<const float4*>(a.partial)
+                                           : own        ? from1 + (long long)(i - r.parts[0]) * (PrefixShape<DIM>::STORE * (DIM / 4))
+                                                        : from0 + (long long)i * (PrefixShape<DIM>::STORE * (DIM / 4));
+                const int next = f[u] == 0.0f ? 0 : LANES * (own ? r.rows[1] : r.rows[0]);
+#pragma unroll
+                for (int c = 0; c < CHUNKS; c++) o[u][c] = from[c * next];
             }
 #pragma unroll
-            for (int u = 0; u < AHEAD; u++) {
-                acc.x += f[u] * o[u].x;
-                acc.y += f[u] * o[u].y;
-                acc.z += f[u] * o[u].z;
-                acc.w += f[u] * o[u].w;
-            }
+            for (int u = 0; u < AHEAD; u++)
+                if (f[u] != 0.0f)
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; c++) {
+                        acc[c].x += f[u] * o[u][c].x;
+                        acc[c].y += f[u] * o[u][c].y;
+                        acc[c].z += f[u] * o[u][c].z;
+                        acc[c].w += f[u] * o[u][c].w;
+                    }
         }
-        *reinterpret_cast<uint2*>(out + chunk * 4) = make_uint2(Pair<T>::pack(acc.x * r.inv, acc.y * r.inv), Pair<T>::pack(acc.z * r.inv, acc.w * r.inv));
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++)
+            *reinterpret_cast<uint2*>(out + (chunk + c * LANES) * 4) =
+                make_uint2(Pair<T>::pack(acc[c].x * r.inv, acc[c].y * r.inv), Pair<T>::pack(acc[c].z * r.inv, acc[c].w * r.inv));
     }
 }
 
