@@ -727,7 +727,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     for (int k = 0; k < 16; k++) {
                         const uint64_t e = fma2(both(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), scale2, base2);
                         float p0, p1;
-                        if (k % 4 == 3) {
+                        if (k == 7) {
                             exp2_pair(e, p0, p1);
                         } else {
                             apart(e, p0, p1);
