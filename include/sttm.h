@@ -504,7 +504,7 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream);
 /*
  * Matrix product of 8-bit rows: out[t][n] = x_scale[t] * w_scale[n] * (sum over k of x[t][k] * w[n][k]) + bias[n], the sums
  * exact, one rounding to out's type.  Both operands are [rows][inner] with 16-byte aligned rows; what lies between inner
- * and the row's end does not matter.  Weights are quantized once, by sttm_quantize_rows over their output channels.
+ * and the row's end does not matter.  The memory from out's first row to its last and that of either operand do not overlap.  Weights are quantized once, by sttm_quantize_rows over their output channels.
  */
 typedef struct sttm_matmul_params {
     const int8_t* x;              /* [rows][inner] tokens, 16-byte aligned                         */

@@ -65,13 +65,18 @@ class Answerer:
                 layer["rows"] = {name: decoder.sttm_quantize_rows(layer[name].t().contiguous()) for name in ("qkv", "out", "up", "down")}
         self.norm, self.embed, self.head = one(c.width), mat(c.vocab, c.width) * c.vocab ** 0.5, mat(c.width, c.vocab)
         self.pools: List[cache.PagedCache] = []                  # one per layer, once a video has been watched
+        self.reported: List[torch.Tensor] = []                   # statuses of the 8-bit products of the call under way
         half = c.dim // 2
         self.rotary = cache.Rotary((c.theta ** (-torch.arange(half, dtype=torch.float64) / half)).float().to(device))
 
     def _project(self, layer: dict, name: str, x: torch.Tensor, gated: bool = False) -> torch.Tensor:
         """``x`` (gated: ``silu(a) * b`` of rows ``[a | b]``) times one of a layer's weights."""
         if self.cfg.int8:
-            return decoder.sttm_quant_matmul(decoder.sttm_quantize_rows(x, gated), layer["rows"][name], self.cfg.dtype)
+            rows = layer["rows"][name]
+            quantize = decoder.QuantizePlan(rows.q.shape[1], self.cfg.dtype, x.shape[0], gated, self.device)
+            product = decoder.MatmulPlan(rows, self.cfg.dtype, x.shape[0])
+            self.reported += [quantize.status, product.status]
+            return product.run(quantize.run(x))
         if gated:
             gate, up = x.chunk(2, -1)
             x = F.silu(gate) * up
@@ -104,7 +109,7 @@ class Answerer:
         x, positions = merged.out_feats[:n], merged.out_pos[:n]
         offsets = torch.tensor([0, n], device=self.device)
         self.pools, pools = [], []
-        statuses = [merged.device_status]
+        statuses, self.reported = [merged.device_status], []
         for layer in self.layers:
             pool = cache.empty_cache(1, n, c.kv_heads, c.dim, c.page, c.dtype, self.device)
             q, k, v = self._qkv(layer, x)
@@ -116,7 +121,7 @@ class Answerer:
             ks, vs = (t.transpose(1, 2).reshape(-1, c.kv_heads, c.dim)[:n].transpose(0, 1).unsqueeze(0) for t in (pool.k, pool.v))
             att = F.scaled_dot_product_attention(q.transpose(0, 1).unsqueeze(0), ks, vs, is_causal=True, enable_gqa=True)
             x = self._rest(layer, x, att[0].transpose(0, 1))
-        _check_status("Answerer.watch", statuses)
+        _check_status("Answerer.watch", statuses + self.reported)
         self.pools = pools
         return n
 
@@ -199,7 +204,7 @@ class Answerer:
         pools = self._question_caches(n, length + answer_tokens)
         lengths = torch.full((n,), self.rows, dtype=torch.int32, device=self.device)
         state = self._state(pools, lengths, keep is not None)
-        statuses = self._statuses(state)
+        statuses, self.reported = self._statuses(state), []
         pos = self.next_position
         for i in range(length):
             logits = self._step(questions[:, i], pos, state)
@@ -223,7 +228,7 @@ class Answerer:
                 logits = self._step(tokens, pos, state)
                 pos += 1
         self.logits = logits
-        _check_status("Answerer.ask", statuses)
+        _check_status("Answerer.ask", statuses + self.reported)
         return torch.stack(answers, 1)
 
 

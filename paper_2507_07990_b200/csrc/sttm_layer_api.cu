@@ -151,11 +151,13 @@ sttm_status launch_matmul(const MatmulArgs& a, const MatmulPlan& pl, const CUten
     return s != STTM_OK ? s : launch(k_quant_matmul<T, NT>, pl.grid, kMatThreads, smem, pl.cluster > 1 ? pl.cluster : 0, stream, a, ma, mb);
 }
 
+bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+}
 // Do two arrays of `rows` rows share memory, other than one in the other's place?
 bool clash(const void* out, long long out_row, const void* in, long long in_row, long long rows, long long width) {
     if (out == nullptr || in == nullptr || (out == in && (out_row == in_row || rows == 1))) return false;
-    const uintptr_t o = (uintptr_t)out, i = (uintptr_t)in;
-    return o < i + (uintptr_t)((rows - 1) * in_row + width) && i < o + (uintptr_t)((rows - 1) * out_row + width);
+    return overlap(out, (rows - 1) * out_row + width, in, (rows - 1) * in_row + width);
 }
 
 }  // namespace
@@ -242,6 +244,8 @@ sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream) {
     if (p->x == nullptr || p->x_scale == nullptr || p->out == nullptr || misaligned(p->x, 16) || p->x_row % 16 != 0 || p->x_row < p->inner) return STTM_ERR_ARG;
     const int e = p->out_dtype == STTM_F32 ? 4 : 2;
     if (misaligned(p->out, e) || (p->rows > 1 && (p->out_row < p->outer || p->out_row > LLONG_MAX / 4 / p->rows))) return STTM_ERR_ARG;
+    const long long span = (p->rows - 1) * (p->rows > 1 ? p->out_row : 0) * e + (long long)p->outer * e;
+    if (overlap(p->out, span, p->x, (p->rows - 1) * p->x_row + p->inner) || overlap(p->out, span, p->w, (p->outer - 1ll) * p->w_row + p->inner)) return STTM_ERR_ARG;
     const MatmulPlan pl = plan_matmul(p);
     if (pl.a_tiles * pl.b_tiles > INT_MAX / 8) return STTM_ERR_UNSUPPORTED;
     MatmulArgs a = {};

@@ -178,6 +178,14 @@ def test_quant_matmul(rows, inner, outer):
     check_matmul(x, w, None, layer.sttm_quant_matmul(x, w, torch.bfloat16))
 
 
+@pytest.mark.parametrize("rows,inner,outer", [(20, 256, 50001), (3, 3584, 40000), (700, 384, 20000)])
+def test_more_tiles_than_blocks(rows, inner, outer):
+    # blocks go from tile to tile
+    gen = torch.Generator().manual_seed(outer)
+    x, w = quant(gen, rows, inner), quant(gen, outer, inner)
+    check_matmul(x, w, None, layer.sttm_quant_matmul(x, w, torch.bfloat16))
+
+
 def test_the_largest_sums_are_exact():
     inner = 131056
     x = layer.QuantRows(torch.full((3, inner), -128, dtype=torch.int8).cuda(), torch.ones(3).cuda())

@@ -69,7 +69,7 @@ def test_bad_matmul_arguments():
     for kw, code in [(dict(rows=-1), ARG), (dict(inner=0), ARG), (dict(outer=0), ARG), (dict(out_dtype=7), ARG), (dict(x=None), ARG), (dict(w=None), ARG),
                      (dict(x_scale=None), ARG), (dict(w_scale=None), ARG), (dict(out=None), ARG), (dict(x=AT + 8), ARG), (dict(w=AT + 8), ARG),
                      (dict(x_row=72), ARG), (dict(w_row=72), ARG), (dict(x_row=48), ARG), (dict(w_row=48), ARG), (dict(out_row=31), ARG),
-                     (dict(out=AT + 1), ARG), (dict(bias=AT + 2), ARG), (dict(inner=131057, x_row=131072, w_row=131072), UNSUPPORTED)]:
+                     (dict(out=AT + 1), ARG), (dict(bias=AT + 2), ARG), (dict(out=AT), ARG), (dict(out=AT + 1024), ARG), (dict(inner=131057, x_row=131072, w_row=131072), UNSUPPORTED)]:
         assert lib.sttm_quant_matmul(C.byref(matmul(**kw)), None) == code, kw
     assert lib.sttm_quant_matmul(None, None) == ARG
     assert lib.sttm_quant_matmul(C.byref(matmul(rows=0)), None) == 0
