@@ -809,6 +809,14 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             if (there && (pair || set == 0)) a.stats[store + row] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
         }
+        // A warp whose wait ran out has left a piece before the barriers at which the sets meet: the others wait for it there, in this piece and
+        // in those to come.
+        if (SETS == 2 && timed_out) {
+            do {
+                if (!walk.pair(a))
+                    for (int i = 0; i < 3; i++) named_sync(1, 256);
+            } while (walk.next(a));
+        }
     }
     tc_fence_before();
     __syncthreads();
