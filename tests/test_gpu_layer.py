@@ -261,3 +261,43 @@ def test_refusals_of_the_plans():
     with pytest.raises(binding.SttmError):
         mat.run(layer.QuantRows(odd[8:264].view(4, 64), w.scale[:4].contiguous()))
     assert mat.run(quant(gen, 0, 64)).shape == (0, 10) and plan.run(x[:0]).out.shape == (0, 64)
+
+
+def test_offsets_beyond_32_bits():
+    # more than 2^31 elements; the last rows are looked at
+    rows, width = 2 ** 31 // 4096 + 300, 4096
+    x = torch.empty((rows, width), dtype=torch.bfloat16, device="cuda").fill_(0.5)
+    gen = torch.Generator().manual_seed(9)
+    x[-3:] = torch.randn((3, width), generator=gen).bfloat16().cuda()
+    w = (1 + 0.3 * torch.randn(width, generator=gen)).cuda()
+    plan = layer.NormPlan(width, torch.bfloat16, rows, pre_norm=w, eps=1e-5)
+    got = plan.run(x, x)
+    last = layer.NormOutput(got.sum[-3:], got.out[-3:], None)
+    check_norm(last, x[-3:], x[-3:], None, [], 1.0, w, 1e-5, False)
+    q = layer.sttm_quantize_rows(x)
+    y = x[-3:].double()
+    step = y.abs().amax(1, keepdim=True) / 127
+    assert not ((layer.QuantRows(q.q[-3:], q.scale[-3:]).dequantized().double() - y).abs() > step * (0.5 + 127 * 2.0 ** -17)).any()
+    del plan, got, x
+    out = layer.sttm_quant_matmul(q, layer.QuantRows(torch.ones((4100, width), dtype=torch.int8, device="cuda"), torch.ones(4100, device="cuda")), torch.bfloat16)
+    assert out.numel() > 2 ** 31
+    want = layer.QuantRows(q.q[-3:], q.scale[-3:]).dequantized().double().sum(1, keepdim=True)
+    assert not ((out[-3:].double() - want).abs() > 2.0 ** -8 * want.abs() + 1e-4).any() and not ((out[:3] - out[3]).abs() > 0).any()
+
+
+def test_plans_on_two_streams():
+    gen = torch.Generator().manual_seed(10)
+    rows = [40, 2000]
+    xs = [rows_of(gen, n, 1024, torch.bfloat16) for n in rows]
+    w = quant(gen, 512, 1024)
+    plans = [(layer.QuantizePlan(1024, torch.bfloat16, n), layer.MatmulPlan(w, torch.bfloat16, n)) for n in rows]
+    streams = [torch.cuda.Stream() for _ in rows]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, (quantize, product), stream in zip(xs, plans, streams):
+            with torch.cuda.stream(stream):
+                product.run(quantize.run(x))
+    torch.cuda.synchronize()
+    for n, (quantize, product) in zip(rows, plans):
+        check_matmul(quantize.rows, w, None, product.out)
+        assert int(quantize.status) == int(product.status) == 0

@@ -240,3 +240,32 @@ def test_one_call_and_refusals_of_the_plan():
             p["q"][:, :3], p["row_offsets"], p["prefix_lengths"], p["lengths"])
     nothing = plan.run(p["q"][:0], torch.zeros_like(p["row_offsets"]), p["prefix_lengths"], p["lengths"])
     assert nothing.out.shape[0] == 0
+
+
+def test_offsets_beyond_32_bits():
+    # pools of more than 2^31 elements; the sequences' pages lie at their ends
+    gen = torch.Generator().manual_seed(14)
+    p = problem(14, lens=(150,), groups=(2,), new=(2, 1), held=(20, 0), page=64)
+    pages = 2 ** 31 // (2 * 64 * 128) + 40
+    for name in ("pre", "mine"):
+        k, v, table = p[name]
+        big = [torch.empty((pages, 2, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        where = pages - 1 - torch.randperm(30, generator=gen)[:k.shape[0]].cuda()
+        for to, small in zip(big, (k, v)):
+            to[where] = small
+        p[name] = [*big, where[table.long()].to(torch.int32)]
+        assert int(p[name][2].min()) * 2 * 64 * 128 > 2 ** 31
+    check(p, run(p))
+
+
+def test_two_plans_on_two_streams():
+    a, b = problem(15, lens=(700,), new=(3, 9), held=(40, 0)), problem(16, dtype="f16", dim=64, lens=(900,), new=(30, 2), held=(0, 7))
+    plans, streams = [plan_of(p) for p in (a, b)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for p, plan, stream in zip((a, b), plans, streams):
+            with torch.cuda.stream(stream):
+                r = run(p, plan)
+    torch.cuda.synchronize()
+    for p, plan in zip((a, b), plans):
+        check(p, prefix.PrefixOutput(plan.out[:p["q"].shape[0]], plan.lse[:p["q"].shape[0]], plan.status))
