@@ -373,7 +373,13 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         const int e = e0 + tid;
         x = PrefixEntry{};
         if (e < entries) x = prefix_entry<DIM>(a, e, bits);
-        const long long s = steps_of(a, x), r = rows_of(a, x), si = warp_scan(s, lane), ri = warp_scan(r, lane);
+        const long long s = steps_of(a, x), r = rows_of(a, x);
+        long long si = s, ri = r;
+        const int busy = min(WARPS, (entries - e0 + 31) / 32);  // warps that have entries
+        if (warp < busy) {
+            si = warp_scan(s, lane);
+            ri = warp_scan(r, lane);
+        }
         if (e0 > 0) __syncthreads();                            // (scan has been read)
         if (lane == 31) {
             scan[warp] = si;
@@ -382,7 +388,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         const int bad = __syncthreads_or(bits & kStatusArg);
         x.step0 = steps + si - s;
         x.row0 = rows + ri - r;
-        for (int w = 0; w < WARPS; w++) {
+        for (int w = 0; w < busy; w++) {
             const long long sw = scan[w], rw = scan[16 + w];
             if (w < warp) {
                 x.step0 += sw;
@@ -489,7 +495,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             };
             look_up(page[0], place[0]);
             look_up(page[1], place[1]);
-            if (part == 0) {
+            if (part == kCopyWarps - 1) {                       // (it has the fewest boxes)
                 if (p > 0 && !mbar_wait_near(q_empty, p - 1, timed_out)) break;
                 if (lane == 0) {
                     const int sets = pair ? 2 : 1, q_bytes = a.block_tokens * a.group * 128;
@@ -832,9 +838,12 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
 constexpr int kPrefixJoinThreads = 256;
 constexpr int kJoinParts = 320;                                 // pieces of a row at most: two entries' over all CTAs
 
-// A block puts ROWS rows (token, query head of one KV head) together: 8 where rows are few and their pieces many, else 32.  First a part
-// of a warp per row finds the row's pieces and their weights; then a thread takes four channels of a row, rows beside each
-// other as the pieces store them.
+// A block puts ROWS rows (token, query head of one KV head) together: 32, or, where rows are few and their pieces many, 8, and then eight chunks
+// of four channels of them, the pieces shared between four groups of threads.  First a part of a warp per row finds the row's pieces and
+// their weights; then a thread takes four channels of a row, rows beside each other as the pieces store them.  Dependent reads bound it: a token's
+// entries, where they lie, m and l, O.
+__host__ __device__ constexpr int prefix_join_split(int dim, int rows) { return rows == 8 ? dim / 32 : 1; }     // blocks per rows
+
 template <typename T, int DIM, int ROWS>
 __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid_constant__ PrefixArgs a) {
     constexpr int LANES = kPrefixJoinThreads / ROWS;            // per row
@@ -848,7 +857,9 @@ __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid
     wait_for_prior_kernel();
     let_next_kernel_start();
     const uint32_t per_kv = (uint32_t)a.rows * a.group, blocks = (per_kv + ROWS - 1) / ROWS;       // (below 2^31)
-    const uint32_t kv = blockIdx.x / blocks, row0 = (blockIdx.x - kv * blocks) * ROWS;
+    constexpr uint32_t SPLIT = prefix_join_split(DIM, ROWS);
+    const uint32_t split = blockIdx.x % SPLIT, at_block = blockIdx.x / SPLIT;
+    const uint32_t kv = at_block / blocks, row0 = (at_block - kv * blocks) * ROWS;
     {
         const int k = threadIdx.x / LANES, lane = threadIdx.x % LANES;
         const uint32_t token = (row0 + k) / (uint32_t)a.group;
@@ -899,17 +910,59 @@ __global__ void __launch_bounds__(kPrefixJoinThreads) k_prefix_join(const __grid
         if (!used || head.total < 0) r.parts[0] = -1;           // (bad offsets: nothing is written)
         if (lane == 0) {
             found[k] = r;
-            if (r.parts[0] >= 0 && a.lse != nullptr)
+            if (r.parts[0] >= 0 && a.lse != nullptr && split == 0)
                 a.lse[(long long)token * a.q_heads + kv * a.group + g] = total == 0.0f ? -INFINITY : (r.top + log2f(total)) * 0.69314718055994531f;
         }
     }
     __syncthreads();
     const int k = threadIdx.x % ROWS;
     const Row r = found[k];
-    if (r.parts[0] < 0) return;
-    const int n = r.parts[0] + r.parts[1];
+    const int n = r.parts[0] < 0 ? 0 : r.parts[0] + r.parts[1];
     const uint32_t token = (row0 + k) / (uint32_t)a.group;
     uint16_t* const out = a.out + ((long long)token * a.q_heads + kv * a.group + (row0 + k - token * a.group)) * DIM;
+    if constexpr (ROWS == 8) {
+        constexpr int GROUPS = 4, AHEAD = 10;
+        __shared__ float4 parked[GROUPS - 1][64];
+        const int group = threadIdx.x / 64, chunk = split * 8 + threadIdx.x / 8 % 8;
+        const float4 *const from0 = r.from[0] + (long long)chunk * r.rows[0], *const from1 = r.from[1] + (long long)chunk * r.rows[1];
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+        for (int i0 = group; i0 < n; i0 += GROUPS * AHEAD) {
+            float4 o[AHEAD];
+            float f[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) {
+                const int i = i0 + u * GROUPS;
+                f[u] = i < n ? weights[k][i] : 0.0f;
+                // (a piece without tiles has the weight 0: it stored no O)
+                o[u] = *(f[u] == 0.0f         ? reinterpret_cast<const float4*>(a.partial)
+                         : i >= r.parts[0] ? from1 + (long long)(i - r.parts[0]) * (PrefixShape<DIM>::STORE * (DIM / 4))
+                                             : from0 + (long long)i * (PrefixShape<DIM>::STORE * (DIM / 4)));
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++)
+                if (f[u] != 0.0f) {
+                    acc.x += f[u] * o[u].x;
+                    acc.y += f[u] * o[u].y;
+                    acc.z += f[u] * o[u].z;
+                    acc.w += f[u] * o[u].w;
+                }
+        }
+        if (group > 0) parked[group - 1][threadIdx.x % 64] = acc;
+        __syncthreads();
+        if (group > 0 || r.parts[0] < 0) return;
+#pragma unroll
+        for (int g = 0; g < GROUPS - 1; g++) {
+            const float4 o = parked[g][threadIdx.x];
+            acc.x += o.x;
+            acc.y += o.y;
+            acc.z += o.z;
+            acc.w += o.w;
+        }
+        *reinterpret_cast<uint2*>(out + chunk * 4) = make_uint2(Pair<T>::pack(acc.x * r.inv, acc.y * r.inv), Pair<T>::pack(acc.z * r.inv, acc.w * r.inv));
+        return;
+    }
+    if (r.parts[0] < 0) return;
     // CHUNKS chunks of four channels of AHEAD pieces are on their way at a time
     constexpr int CHUNKS = DIM / 4 > LANES ? (DIM / 4 / LANES < 4 ? DIM / 4 / LANES : 4) : 1, AHEAD = 16 / CHUNKS;
 #pragma unroll 1

@@ -32,8 +32,11 @@ sttm_status plan_prefix(const sttm_cache* prefix, const sttm_cache* own, const s
     if (p->rows > INT_MAX - 256 || p->seqs > INT_MAX / 2 || prefix->seqs > INT_MAX / 2) return STTM_ERR_UNSUPPORTED;
     pl->grid = std::min(sm_count(), kJoinParts / 2);
     const long long heads = p->rows * p->q_heads;
+    // Few rows have many pieces each, and leave SMs idle unless several blocks share them; many rows keep every SM busy with 32
+    // rows to a block, which reads each piece's statistics once.  Measured, 8 rows against 32: 56 rows x heads 16.3 us against
+    // 18.9, 448 44.0 against 59.7; 4900 54.6 against 39.7, 6144 147 against 126, 21364 735 against 664.
     pl->join_rows = heads <= pl->grid * 32 ? 8 : 32;
-    pl->join_grid = (p->rows * group + pl->join_rows - 1) / pl->join_rows * prefix->heads;
+    pl->join_grid = (p->rows * group + pl->join_rows - 1) / pl->join_rows * prefix->heads * prefix_join_split(prefix->dim, pl->join_rows);
     if (heads > INT_MAX) return STTM_ERR_UNSUPPORTED;
     // every row once per kind of entry, and every CTA's pieces in a stretch of their own
     const long long rows = pl->grid * 256 + heads * (own != nullptr ? 2 : 1);
