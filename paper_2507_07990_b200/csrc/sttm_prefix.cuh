@@ -62,6 +62,8 @@ struct PrefixEntry {
     int blocks;                   // row blocks per KV head (pairs of 128 rows, or one block whose tiles alternate)
 };
 
+constexpr int kPieces = 4;                                      // worked out ahead
+
 template <int DIM>
 struct PrefixShape {
     static constexpr int SLOTS = DIM == 256 ? 64 : 128;         // per tile
@@ -71,7 +73,7 @@ struct PrefixShape {
     static constexpr int RING = DIM == 64 ? 10 : 5;
     static constexpr int THREADS = SETS * 128 + 128;            // softmax warps, one that issues the products, three that copy
     static constexpr uint32_t O_COL = 256;                      // S at columns 0 and 128, O from here on
-    static constexpr int BARS = 2 + 2 * RING + 8;
+    static constexpr int BARS = 2 + 2 * RING + 8 + 2 * kPieces;
     static constexpr size_t SMEM = (size_t)SETS * QBLOCK + (size_t)RING * TILE + BARS * 8 + 16 + 64 * 8 + 128 * 8 + 1024;
     static constexpr int STORE = SETS * 128;                    // stored rows of a piece at most
 };
@@ -157,15 +159,32 @@ __device__ __forceinline__ long long warp_scan(long long v, int lane) {
     return v;
 }
 
-// A CTA's pieces, one after the other; every warp walks them for itself.
+// What a CTA has of an item, as one warp works it out for the others, in shared memory (every warp for itself, with the walk's state in the
+// softmax warps' registers: 16 questions on 55724 slots 659 us against 630, 96 answers on 6 videos 125 against 116).
+struct Piece {
+    long long first, store;       // the entry's first token; stored row of the piece's first
+    long long step0, step, end;   // steps before the entry, before the next piece, before the next CTA's first
+    int tokens, len;              // of the entry
+    int u0, u1;                   // tiles
+    int head, block, at;          // at: entry
+    bool own, pair, there;        // pair: two blocks of rows, else one, of whose tiles the sets take every other; there: not behind the last
+    __device__ __forceinline__ int tiles() const { return u1 - u0; }
+    // rows (token, query head) of a set's block, and the first of them in memory
+    __device__ __forceinline__ int set_rows(const PrefixArgs& a, int set) const {
+        return min(a.block_tokens, max(0, tokens - (block * (pair ? 2 : 1) + set) * a.block_tokens)) * a.group;
+    }
+    __device__ __forceinline__ long long set_store(const PrefixArgs& a, int set) const { return store + set * a.block_tokens * a.group; }
+};
+
 template <int DIM>
 struct PieceWalk {
     PrefixEntry e;
-    int at;                                                     // entry
+    int at;
     long long step, end;
-    int item, head, block, u0, u1;
-    __device__ __forceinline__ bool next(const PrefixArgs& a) {
-        if (step >= end) return false;
+    __device__ __forceinline__ Piece next(const PrefixArgs& a) {
+        Piece p;
+        p.there = step < end;
+        if (!p.there) return p;
         int32_t bits = 0;
         while (step >= e.step0 + steps_of(a, e)) {
             const long long s = e.step0 + steps_of(a, e), r = e.row0 + rows_of(a, e);
@@ -174,30 +193,30 @@ struct PieceWalk {
             e.row0 = r;
         }
         const long long in = step - e.step0;
-        item = (int)quotient(in, e.units);
+        const int item = (int)quotient(in, e.units);
         const int from = (int)(in - (long long)item * e.units), to = (int)min((long long)e.units, from + (end - step));
         step += to - from;
-        u0 = max(0, from - kPieceSteps);
-        u1 = max(0, to - kPieceSteps);
-        head = item / e.blocks;
-        block = item - head * e.blocks;
-        if (is_own(a)) {
+        p.first = e.first;
+        p.step0 = e.step0;
+        p.step = step;
+        p.end = end;
+        p.tokens = e.tokens;
+        p.len = e.len;
+        p.at = at;
+        p.own = at >= a.prefix.seqs;
+        p.pair = !alternates<DIM>(a, e);
+        p.u0 = max(0, from - kPieceSteps);
+        p.u1 = max(0, to - kPieceSteps);
+        p.head = item / e.blocks;
+        p.block = item - p.head * e.blocks;
+        const int per = (p.pair ? 2 : 1) * a.block_tokens;
+        if (p.own) {
             // tiles behind the last slot that the block's last token sees hold nothing for it
-            const int per = (alternates<DIM>(a, e) ? 1 : 2) * a.block_tokens, last = min(e.tokens, (block + 1) * per);
-            const int seen = max(0, e.len - e.tokens + last);
-            u1 = max(u0, min(u1, (seen + PrefixShape<DIM>::SLOTS - 1) / PrefixShape<DIM>::SLOTS));
+            const int last = min(e.tokens, (p.block + 1) * per), seen = max(0, e.len - e.tokens + last);
+            p.u1 = max(p.u0, min(p.u1, (seen + PrefixShape<DIM>::SLOTS - 1) / PrefixShape<DIM>::SLOTS));
         }
-        return true;
-    }
-    __device__ __forceinline__ bool is_own(const PrefixArgs& a) const { return at >= a.prefix.seqs; }
-    __device__ __forceinline__ int tiles() const { return u1 - u0; }
-    __device__ __forceinline__ bool pair(const PrefixArgs& a) const { return !alternates<DIM>(a, e); }
-    // rows (token, query head) of a set's block, and the first of them in memory
-    __device__ __forceinline__ int set_rows(const PrefixArgs& a, int set) const {
-        return min(a.block_tokens, max(0, e.tokens - (block * (pair(a) ? 2 : 1) + set) * a.block_tokens)) * a.group;
-    }
-    __device__ __forceinline__ long long store(const PrefixArgs& a, int set) const {
-        return (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + ((long long)head * e.tokens + (long long)(block * (pair(a) ? 2 : 1) + set) * a.block_tokens) * a.group;
+        p.store = (long long)blockIdx.x * PrefixShape<DIM>::STORE + e.row0 + ((long long)p.head * e.tokens + (long long)p.block * per) * a.group;
+        return p;
     }
 };
 
@@ -332,8 +351,11 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     unsigned char* rest = smem + SETS * Shape::QBLOCK + RING * TILE;
     const uint32_t q_full = smem_u32(rest), q_empty = q_full + 8, full = q_full + 16, empty = full + 8 * RING;
     const uint32_t s_full = empty + 8 * RING, p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16;
+    const uint32_t piece_full = o_full + 16, piece_empty = piece_full + 8 * kPieces;
     uint32_t* tmem_word = reinterpret_cast<uint32_t*>(rest + Shape::BARS * 8);
     long long* scan = reinterpret_cast<long long*>(rest + Shape::BARS * 8 + 16);        // [64]
+    Piece* const pieces = reinterpret_cast<Piece*>(scan);       // [kPieces], once the shares are known
+    static_assert(sizeof(Piece) * kPieces <= 40 * sizeof(long long) && sizeof(PrefixEntry) <= 8 * sizeof(long long), "scan's places");
     float2* stat = reinterpret_cast<float2*>(scan + 64);        // [128] m and l of a row in the second set
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -350,6 +372,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             mbar_init(p_half + 8 * b, 4);
             mbar_init(p_full + 8 * b, 4);
             mbar_init(o_full + 8 * b, 1);
+        }
+        for (int i = 0; i < kPieces; i++) {
+            mbar_init(piece_full + 8 * i, 1);
+            mbar_init(piece_empty + 8 * i, WARPS - 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -408,12 +434,12 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     if (blockIdx.x == 0 && bits) raise_status(a.status, bits);
     const long long total = bad ? 0 : steps, share = quotient(total + gridDim.x - 1, gridDim.x);
     if (blockIdx.x == 0 && tid == 0) *a.head = PrefixHead{bad ? -1 : total, share};
-    PieceWalk<DIM> walk;
+    PieceWalk<DIM> walk = {};
     walk.step = min(total, (long long)blockIdx.x * share);
     walk.end = min(total, walk.step + share);
+    PrefixEntry* found = reinterpret_cast<PrefixEntry*>(scan + 40);
+    int* found_at = reinterpret_cast<int*>(scan + 48);
     if (total > 0) {
-        PrefixEntry* found = reinterpret_cast<PrefixEntry*>(scan + 40);
-        int* found_at = reinterpret_cast<int*>(scan + 48);
         const bool once = entries <= Shape::THREADS;            // x is still there
         steps = rows = 0;
         for (int e0 = 0; e0 < entries; e0 += Shape::THREADS) {
@@ -432,16 +458,34 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 for (int i = once ? blockIdx.x : 0; i < x.tokens; i += once ? gridDim.x : 1) (e < a.prefix.seqs ? a.prefix_of : a.own_of)[x.first + i] = e;
             if (blockIdx.x != 0 && !once && steps > walk.step) break;       // (the same for the whole CTA)
         }
-        __syncthreads();
-        if (walk.step < walk.end) {
-            walk.e = *found;
-            walk.at = *found_at;
-        }
+    }
+    __syncthreads();
+    if (walk.step < walk.end) {
+        walk.e = *found;
+        walk.at = *found_at;
     }
 
     // 384 threads are launched with 168 registers each (64512).  The softmax warps hold a row of 128 logits: they take 208, for
     // which the third warpgroup goes down to 88 (128 * 88 + 256 * 208 = 64512).
     bool timed_out = false;
+    // The last copy warp (it has the fewest boxes of a tile) works out the pieces, one ahead of its own copies, and puts them into shared memory.
+    auto publish = [&](int i) -> bool {
+        const Piece next = walk.next(a);
+        if (i >= kPieces && !mbar_wait_near(piece_empty + 8 * (i % kPieces), i / kPieces - 1, timed_out)) return false;
+        if (lane == 0) {
+            pieces[i % kPieces] = next;
+            mbar_arrive(piece_full + 8 * (i % kPieces));
+        }
+        __syncwarp();
+        return true;
+    };
+    auto piece = [&](int i, Piece& now, bool mine) -> bool {
+        if (!mbar_wait_near(piece_full + 8 * (i % kPieces), i / kPieces, timed_out)) return false;
+        now = pieces[i % kPieces];
+        __syncwarp();
+        if (lane == 0 && !mine) mbar_arrive(piece_empty + 8 * (i % kPieces));
+        return now.there;
+    };
     if (warp >= COPY_WARP) {
         if constexpr (SETS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp != MMA_WARP) {
@@ -449,22 +493,26 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         // Issuing a tensor copy keeps a warp busy for some 80 cycles whatever its size, and small pages make many of them: the
         // boxes of a tile (a box of slots, 64 channels) are shared between three warps, one box to a lane.
         const int part = warp == COPY_WARP ? 0 : warp - MMA_WARP;
-        int n = 0, p = 0;                                       // ring slots and pieces taken up so far
-        while (!timed_out && walk.next(a)) {
-            const int tiles = walk.tiles();
+        int n = 0, p = 0;                                       // ring slots and pieces with tiles taken up so far
+        const bool walks = part == kCopyWarps - 1;
+        Piece now;
+        if (walks) publish(0);
+        for (int i = 0;; i++) {
+            if (!piece(i, now, walks) || (walks && !publish(i + 1))) break;
+            const int tiles = now.tiles();
             if (tiles == 0) continue;
-            const bool pair = walk.pair(a);
-            const int own = walk.is_own(a);
+            const bool pair = now.pair;
+            const int own = now.own;
             const CacheView& c = own ? a.own : a.prefix;
             const int box = a.page_box[own], page_slots = c.page, pages = (int)c.pages;
-            const int32_t* table = c.table + (own ? walk.at - a.prefix.seqs : walk.at) * c.table_stride;
+            const int32_t* table = c.table + (own ? now.at - a.prefix.seqs : now.at) * c.table_stride;
             const int at = lane * kCopyWarps + part, in_tile = at / HALVES * box, half = at % HALVES;
             const bool copies = in_tile < SLOTS;
             // Page and place in it of this lane's box, by the tile's number modulo four; looked up two tiles ahead.  (-1: the box lies
             // behind the last slot.  It is not copied: logits there are masked, values cleared.  `pages`, beyond the pool: zeros.)
             int page[4], place[4];
-            const int slot0 = walk.u0 * SLOTS + in_tile, by_pages = SLOTS / page_slots, by_slots = SLOTS % page_slots;
-            int left = walk.e.len - slot0, stretch = slot0 / page_slots, spot = slot0 - stretch * page_slots;     // of the tile looked up next
+            const int slot0 = now.u0 * SLOTS + in_tile, by_pages = SLOTS / page_slots, by_slots = SLOTS % page_slots;
+            int left = now.len - slot0, stretch = slot0 / page_slots, spot = slot0 - stretch * page_slots;     // of the tile looked up next
             auto look_up = [&](int& pg, int& pl) {
                 pg = -1;
                 pl = spot;
@@ -492,22 +540,22 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                         raise_status(a.status, kStatusArg);
                         pg = pages;
                     }
-                    copy_slots(to + s * TILE, map, pl, half, walk.head, pg, full + 8 * s);
+                    copy_slots(to + s * TILE, map, pl, half, now.head, pg, full + 8 * s);
                 }
                 n++;
                 return true;
             };
             look_up(page[0], place[0]);
             look_up(page[1], place[1]);
-            if (part == kCopyWarps - 1) {                       // (it has the fewest boxes)
+            if (walks) {
                 if (p > 0 && !mbar_wait_near(q_empty, p - 1, timed_out)) break;
                 if (lane == 0) {
                     const int sets = pair ? 2 : 1, q_bytes = a.block_tokens * a.group * 128;
                     mbar_expect_tx(q_full, sets * HALVES * q_bytes);
                     for (int t = 0; t < sets; t++)
                         for (int h = 0; h < HALVES; h++)
-                            copy_queries(qmem + t * Shape::QBLOCK + h * (128 * 128), &maps.q, walk.head * a.group, h,
-                                         (int)(walk.e.first + (long long)(walk.block * sets + t) * a.block_tokens), q_full);
+                            copy_queries(qmem + t * Shape::QBLOCK + h * (128 * 128), &maps.q, now.head * a.group, h,
+                                         (int)(now.first + (long long)(now.block * sets + t) * a.block_tokens), q_full);
                 }
                 __syncwarp();
                 p++;
@@ -559,10 +607,11 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             return ok;
         };
-        while (!timed_out && walk.next(a)) {
-            const int tiles = walk.tiles();
+        Piece now;
+        for (int i = 0; piece(i, now, false); i++) {
+            const int tiles = now.tiles();
             if (tiles == 0) continue;
-            const bool pair = walk.pair(a);
+            const bool pair = now.pair;
             // logits of set (place) b
             auto logits = [&](auto place, int set, uint32_t k_slot, bool frees, bool last) {
                 constexpr int b = decltype(place)::value;
@@ -605,7 +654,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             };
             // What lies behind the last slot may be anything: 0 times it must be 0.
             auto clear_tail = [&](int j, uint32_t v_slot) {
-                const int there = walk.e.len - (walk.u0 + j) * SLOTS;
+                const int there = now.len - (now.u0 + j) * SLOTS;
                 if (j + 1 < tiles || there >= SLOTS) return;
                 for (int w = lane; w < (SLOTS - there) * 8 * HALVES; w += 32) {
                     const int h = w / ((SLOTS - there) * 8), u = w - h * (SLOTS - there) * 8;
@@ -673,12 +722,19 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         const uint32_t o_at = tmem + lanes + Shape::O_COL + set * DIM;
         const int tok = row / a.group;
         int s_uses0 = 0, s_uses1 = 0, o_uses = 0;               // logits taken from either place, products into O
-        while (!timed_out && walk.next(a)) {
-            const bool pair = walk.pair(a);
-            const int tiles = walk.tiles(), token = (walk.block * (pair ? 2 : 1) + (pair ? set : 0)) * a.block_tokens + tok;
-            const bool there = tok < a.block_tokens && token < walk.e.tokens;
+        Piece now;
+        now.step0 = walk.e.step0;
+        now.step = walk.step;
+        now.end = walk.end;
+        now.at = walk.at;
+        bool within = false;                                    // a piece whose barriers are to come
+        for (int i = 0; piece(i, now, false); i++) {
+            within = true;
+            const bool pair = now.pair;
+            const int tiles = now.tiles(), token = (now.block * (pair ? 2 : 1) + (pair ? set : 0)) * a.block_tokens + tok;
+            const bool there = tok < a.block_tokens && token < now.tokens;
             // slots that this row sees
-            const int limit = walk.is_own(a) ? min(walk.e.len, walk.e.len - walk.e.tokens + token + 1) : walk.e.len;
+            const int limit = now.own ? min(now.len, now.len - now.tokens + token + 1) : now.len;
             float m = -INFINITY, l = 0.0f;
             const int steps = pair ? 2 * tiles : tiles;
             bool first = true;
@@ -693,7 +749,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tmem_wait_load();
 #pragma unroll
                 for (int i = 0; i < SLOTS / 32; i++) tmem_loaded(v[i]);
-                const int left = limit - (walk.u0 + j) * SLOTS;  // slots of this tile that the row sees
+                const int left = limit - (now.u0 + j) * SLOTS;  // slots of this tile that the row sees
                 if (__any_sync(0xffffffffu, left < SLOTS)) {
 #pragma unroll
                     for (int i = 0; i < SLOTS; i++)
@@ -768,8 +824,8 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             // this piece's O, l and m
             if (!first && !mbar_wait_near(o_full + 8 * set, o_uses - 1, timed_out)) break;
             tc_fence_after();
-            const int rows = walk.set_rows(a, pair ? set : 0);
-            const long long store = walk.store(a, pair ? set : 0);
+            const int rows = now.set_rows(a, pair ? set : 0);
+            const long long store = now.set_store(a, pair ? set : 0);
             float4* const to = reinterpret_cast<float4*>(a.partial + store * DIM) + row;
             if (SETS == 2 && !pair) {
                 // both sets have a part of the same rows, in the same lanes: each puts half of the channels together
@@ -818,14 +874,21 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tc_fence_before();
             }
             if (there && (pair || set == 0)) a.stats[store + row] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
+            within = false;
         }
-        // A warp whose wait ran out has left a piece before the barriers at which the sets meet: the others wait for it there, in this piece and
-        // in those to come.
+        // A warp whose wait ran out has left a piece before the barriers at which the sets meet, or does not learn of the pieces to come: the
+        // others wait for it there.
         if (SETS == 2 && timed_out) {
-            do {
-                if (!walk.pair(a))
-                    for (int i = 0; i < 3; i++) named_sync(1, 256);
-            } while (walk.next(a));
+            auto meet = [] { for (int i = 0; i < 3; i++) named_sync(1, 256); };
+            if (within && !now.pair) meet();
+            int32_t bits = 0;
+            walk.e = prefix_entry<DIM>(a, now.at, bits);
+            walk.e.step0 = now.step0;
+            walk.step = now.step;
+            walk.end = now.end;
+            walk.at = now.at;
+            for (now = walk.next(a); now.there; now = walk.next(a))
+                if (!now.pair) meet();
         }
     }
     tc_fence_before();
