@@ -292,24 +292,6 @@ __device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
     for (int i = 0; i < 32; i += 8)
         asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]));
 }
-// 2^x twice without the special-function unit, for x in [-126, 127) (below: 2^-126): x = n + f with |f| <= 1/2, 2^f by the polynomial
-// of degree 4 whose largest relative error is least (2.6e-6: Remez exchange over [-1/2, 1/2]), n added to the exponent.
-__device__ __forceinline__ void exp2_pair(uint64_t x, float& x0, float& x1) {
-    apart(x, x0, x1);
-    x = both(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f));
-    const uint64_t shift = both(12582912.0f, 12582912.0f);      // 1.5 * 2^23: the sum's lowest bits are n
-    const uint64_t t = add2(x, shift), n = add2(t, both(-12582912.0f, -12582912.0f));
-    const uint64_t f = fma2(n, both(-1.0f, -1.0f), x);
-    uint64_t p = fma2(both(0.009570102f, 0.009570102f), f, both(0.05591786f, 0.05591786f));
-    p = fma2(p, f, both(0.24024744f, 0.24024744f));
-    p = fma2(p, f, both(0.6931218f, 0.6931218f));
-    p = fma2(p, f, both(0.9999993f, 0.9999993f));
-    float t0, t1;
-    apart(t, t0, t1);
-    apart(p, x0, x1);
-    x0 = __uint_as_float(__float_as_uint(x0) + (__float_as_uint(t0) << 23));
-    x1 = __uint_as_float(__float_as_uint(x1) + (__float_as_uint(t1) << 23));
-}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -793,13 +775,9 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     for (int k = 0; k < 16; k++) {
                         const uint64_t e = fma2(both(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), scale2, base2);
                         float p0, p1;
-                        if (k == 7) {
-                            exp2_pair(e, p0, p1);
-                        } else {
-                            apart(e, p0, p1);
-                            p0 = exp2_fast(p0);
-                            p1 = exp2_fast(p1);
-                        }
+                        apart(e, p0, p1);
+                        p0 = exp2_fast(p0);
+                        p1 = exp2_fast(p1);
                         sum[k & 1] = add2(sum[k & 1], both(p0, p1));
                         w[k] = Pair<T>::pack(p0, p1);
                     }
