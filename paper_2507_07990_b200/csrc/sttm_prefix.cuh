@@ -163,7 +163,6 @@ __device__ __forceinline__ long long warp_scan(long long v, int lane) {
 // softmax warps' registers: 16 questions on 55724 slots 659 us against 630, 96 answers on 6 videos 125 against 116).
 struct Piece {
     long long first, store;       // the entry's first token; stored row of the piece's first
-    long long step0, step, end;   // steps before the entry, before the next piece, before the next CTA's first
     int tokens, len;              // of the entry
     int u0, u1;                   // tiles
     int head, block, at;          // at: entry
@@ -197,9 +196,6 @@ struct PieceWalk {
         const int from = (int)(in - (long long)item * e.units), to = (int)min((long long)e.units, from + (end - step));
         step += to - from;
         p.first = e.first;
-        p.step0 = e.step0;
-        p.step = step;
-        p.end = end;
         p.tokens = e.tokens;
         p.len = e.len;
         p.at = at;
@@ -337,7 +333,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     uint32_t* tmem_word = reinterpret_cast<uint32_t*>(rest + Shape::BARS * 8);
     long long* scan = reinterpret_cast<long long*>(rest + Shape::BARS * 8 + 16);        // [64]
     Piece* const pieces = reinterpret_cast<Piece*>(scan);       // [kPieces], once the shares are known
-    static_assert(sizeof(Piece) * kPieces <= 40 * sizeof(long long) && sizeof(PrefixEntry) <= 8 * sizeof(long long), "scan's places");
+    static_assert(sizeof(Piece) * kPieces <= 40 * sizeof(long long) && sizeof(PieceWalk<DIM>) <= 16 * sizeof(long long), "scan's places");
     float2* stat = reinterpret_cast<float2*>(scan + 64);        // [128] m and l of a row in the second set
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -416,11 +412,14 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
     if (blockIdx.x == 0 && bits) raise_status(a.status, bits);
     const long long total = bad ? 0 : steps, share = quotient(total + gridDim.x - 1, gridDim.x);
     if (blockIdx.x == 0 && tid == 0) *a.head = PrefixHead{bad ? -1 : total, share};
-    PieceWalk<DIM> walk = {};
+    PieceWalk<DIM> walk;                                        // (without work of its own it stays where it is)
     walk.step = min(total, (long long)blockIdx.x * share);
     walk.end = min(total, walk.step + share);
-    PrefixEntry* found = reinterpret_cast<PrefixEntry*>(scan + 40);
-    int* found_at = reinterpret_cast<int*>(scan + 48);
+    PieceWalk<DIM>* const start = reinterpret_cast<PieceWalk<DIM>*>(scan + 40);
+    if (tid == 0) {
+        start->step = walk.step;
+        start->end = walk.end;
+    }
     if (total > 0) {
         const bool once = entries <= Shape::THREADS;            // x is still there
         steps = rows = 0;
@@ -431,8 +430,8 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             const int e = e0 + tid;
             if (e < entries && x.step0 <= walk.step && walk.step < x.step0 + steps_of(a, x)) {
-                *found = x;
-                *found_at = e;
+                start->e = x;
+                start->at = e;
             }
             if (blockIdx.x == 0 && e < entries) a.entries[e] = x;
             // the tokens' entries, shared between the CTAs (one does it where entries are so many that the others do not see them all)
@@ -442,10 +441,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         }
     }
     __syncthreads();
-    if (walk.step < walk.end) {
-        walk.e = *found;
-        walk.at = *found_at;
-    }
+    walk = *start;
 
     // 384 threads are launched with 168 registers each (64512).  The softmax warps hold a row of 128 logits: they take 208, for
     // which the third warpgroup goes down to 88 (128 * 88 + 256 * 208 = 64512).
@@ -461,12 +457,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         __syncwarp();
         return true;
     };
-    auto piece = [&](int i, Piece& now, bool mine) -> bool {
-        if (!mbar_wait_near(piece_full + 8 * (i % kPieces), i / kPieces, timed_out)) return false;
-        now = pieces[i % kPieces];
+    auto there_is = [&](int i) -> bool { return mbar_wait_near(piece_full + 8 * (i % kPieces), i / kPieces, timed_out) && pieces[i % kPieces].there; };
+    auto done_with = [&](int i) {
         __syncwarp();
-        if (lane == 0 && !mine) mbar_arrive(piece_empty + 8 * (i % kPieces));
-        return now.there;
+        if (lane == 0) mbar_arrive(piece_empty + 8 * (i % kPieces));
     };
     if (warp >= COPY_WARP) {
         if constexpr (SETS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
@@ -477,10 +471,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         const int part = warp == COPY_WARP ? 0 : warp - MMA_WARP;
         int n = 0, p = 0;                                       // ring slots and pieces with tiles taken up so far
         const bool walks = part == kCopyWarps - 1;
-        Piece now;
         if (walks) publish(0);
-        for (int i = 0;; i++) {
-            if (!piece(i, now, walks) || (walks && !publish(i + 1))) break;
+        for (int i = 0; there_is(i) && (!walks || publish(i + 1)); i++) {
+            const Piece now = pieces[i % kPieces];
+            if (!walks) done_with(i);
             const int tiles = now.tiles();
             if (tiles == 0) continue;
             const bool pair = now.pair;
@@ -589,8 +583,9 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             }
             return ok;
         };
-        Piece now;
-        for (int i = 0; piece(i, now, false); i++) {
+        for (int i = 0; there_is(i); i++) {
+            const Piece now = pieces[i % kPieces];
+            done_with(i);
             const int tiles = now.tiles();
             if (tiles == 0) continue;
             const bool pair = now.pair;
@@ -704,19 +699,14 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         const uint32_t o_at = tmem + lanes + Shape::O_COL + set * DIM;
         const int tok = row / a.group;
         int s_uses0 = 0, s_uses1 = 0, o_uses = 0;               // logits taken from either place, products into O
-        Piece now;
-        now.step0 = walk.e.step0;
-        now.step = walk.step;
-        now.end = walk.end;
-        now.at = walk.at;
-        bool within = false;                                    // a piece whose barriers are to come
-        for (int i = 0; piece(i, now, false); i++) {
-            within = true;
+        int at = 0;                                             // piece
+        for (; there_is(at); at++) {
+            const Piece& now = pieces[at % kPieces];
             const bool pair = now.pair;
             const int tiles = now.tiles(), token = (now.block * (pair ? 2 : 1) + (pair ? set : 0)) * a.block_tokens + tok;
             const bool there = tok < a.block_tokens && token < now.tokens;
-            // slots that this row sees
-            const int limit = now.own ? min(now.len, now.len - now.tokens + token + 1) : now.len;
+            // slots that this row sees, of the piece's
+            const int limit = (now.own ? min(now.len, now.len - now.tokens + token + 1) : now.len) - now.u0 * SLOTS;
             float m = -INFINITY, l = 0.0f;
             const int steps = pair ? 2 * tiles : tiles;
             bool first = true;
@@ -731,7 +721,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tmem_wait_load();
 #pragma unroll
                 for (int i = 0; i < SLOTS / 32; i++) tmem_loaded(v[i]);
-                const int left = limit - (now.u0 + j) * SLOTS;  // slots of this tile that the row sees
+                const int left = limit - j * SLOTS;             // slots of this tile that the row sees
                 if (__any_sync(0xffffffffu, left < SLOTS)) {
 #pragma unroll
                     for (int i = 0; i < SLOTS; i++)
@@ -852,21 +842,18 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tc_fence_before();
             }
             if (there && (pair || set == 0)) a.stats[store + row] = make_float2(m == -INFINITY ? -INFINITY : m * a.scale_log2 - kWeightBias<T>, l);
-            within = false;
+            done_with(at);
         }
         // A warp whose wait ran out has left a piece before the barriers at which the sets meet, or does not learn of the pieces to come: the
         // others wait for it there.
         if (SETS == 2 && timed_out) {
-            auto meet = [] { for (int i = 0; i < 3; i++) named_sync(1, 256); };
-            if (within && !now.pair) meet();
-            int32_t bits = 0;
-            walk.e = prefix_entry<DIM>(a, now.at, bits);
-            walk.e.step0 = now.step0;
-            walk.step = now.step;
-            walk.end = now.end;
-            walk.at = now.at;
-            for (now = walk.next(a); now.there; now = walk.next(a))
-                if (!now.pair) meet();
+            walk = *start;
+            for (int i = 0;; i++) {
+                const Piece now = walk.next(a);
+                if (!now.there) break;
+                if (i >= at && !now.pair)
+                    for (int k = 0; k < 3; k++) named_sync(1, 256);
+            }
         }
     }
     tc_fence_before();
