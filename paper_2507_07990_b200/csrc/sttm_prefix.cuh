@@ -795,7 +795,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             const int rows = now.set_rows(a, pair ? set : 0);
             const long long store = now.set_store(a, pair ? set : 0);
             float4* const to = reinterpret_cast<float4*>(a.partial + store * DIM) + row;
-            if (SETS == 2 && !pair) {
+            if (SETS == 2 && !pair && tiles > 1) {
                 // both sets have a part of the same rows, in the same lanes: each puts half of the channels together
                 if (set == 1) stat[row] = make_float2(m, l);
                 named_sync(1, 256);
@@ -814,21 +814,17 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     f0 = stat[row].x;
                     f1 = stat[row].y;
                 }
-                if (tiles > 0) {
 #pragma unroll 1
-                    for (int i = set * (DIM / 2); i < (set + 1) * (DIM / 2); i += 32) {
-                        uint32_t o[32], u[32];
-                        tmem_load32(tmem + lanes + Shape::O_COL + i, o);
-                        if (steps > 1) tmem_load32(tmem + lanes + Shape::O_COL + DIM + i, u);
-                        tmem_wait_load();
-                        tmem_loaded(o);
-                        if (steps > 1) {
-                            tmem_loaded(u);
+                for (int i = set * (DIM / 2); i < (set + 1) * (DIM / 2); i += 32) {
+                    uint32_t o[32], u[32];
+                    tmem_load32(tmem + lanes + Shape::O_COL + i, o);
+                    tmem_load32(tmem + lanes + Shape::O_COL + DIM + i, u);
+                    tmem_wait_load();
+                    tmem_loaded(o);
+                    tmem_loaded(u);
 #pragma unroll
-                            for (int k = 0; k < 32; k++) o[k] = __float_as_uint(f0 * __uint_as_float(o[k]) + f1 * __uint_as_float(u[k]));
-                        }
-                        if (there) store32(to + (i / 4) * rows, rows, o);
-                    }
+                    for (int k = 0; k < 32; k++) o[k] = __float_as_uint(f0 * __uint_as_float(o[k]) + f1 * __uint_as_float(u[k]));
+                    if (there) store32(to + (i / 4) * rows, rows, o);
                 }
                 tc_fence_before();
                 named_sync(1, 256);                             // before either set's O is begun again
@@ -851,7 +847,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
             for (int i = 0;; i++) {
                 const Piece now = walk.next(a);
                 if (!now.there) break;
-                if (i >= at && !now.pair)
+                if (i >= at && !now.pair && now.tiles() > 1)
                     for (int k = 0; k < 3; k++) named_sync(1, 256);
             }
         }
