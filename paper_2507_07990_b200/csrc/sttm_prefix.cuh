@@ -10,18 +10,18 @@
 // step of it, as the output is); their sum l is taken before that rounding, in 32 bits.
 //
 // Two row blocks of 128 are in work at a time (of one block, alternate tiles), so that the products of one run beside the
-// exponentials of the other: four warps per block, one that copies (queries, then key and value tiles through a ring) and one
+// exponentials of the other: four warps per block, three that copy (queries, then key and value tiles through a ring) and one
 // that issues the products.  256-channel heads fill tensor memory with one O: there one block's tiles alternate between two
 // places for S.
 //
 // Work is cut into equal shares of steps over all CTAs whatever the lengths are (which the host does not know): entries are the prefixes
 // and then the sequences' own slots; an entry has an item per KV head and block of rows, an item a step per tile of slots and
 // kPieceSteps for what it costs besides (queries in, O out).  What a CTA has of an item is a piece: O, l and m of its rows go to
-// memory, and k_prefix_join puts a row's pieces together.
+// memory, and k_prefix_join puts a row's pieces together.  One of the copy warps works the pieces out for the others.
 //
-// Measured (bf16, 28 / 4 heads of 128): 16 questions of 53 to 42 tokens on 55724 slots 0.66 ms, 565 us of them in the first kernel
-// at full clocks (1080 TFLOP/s, the tensor cores busy 63 % of the time: the chain logits, weights, output of either block
-// bounds it); one answer token each 44 us, 2.6 TB/s (tiles at HBM's rate, then 10 us of start and end and 7 of the join).
+// Measured (bf16, 28 / 4 heads of 128): 16 questions of 53 to 42 tokens on 55724 slots 0.62 to 0.64 ms, 516 to 537 us of them in the first
+// kernel (1140 to 1180 TFLOP/s at 1.6 GHz, the tensor cores busy 69 % of the time, the special-function units 66 %); one answer token
+// each 37 us, 3.1 TB/s (tiles at HBM's rate, then 7 us of start and end and 7 of the join).
 #pragma once
 
 #include <climits>

@@ -33,8 +33,8 @@ sttm_status plan_prefix(const sttm_cache* prefix, const sttm_cache* own, const s
     pl->grid = std::min(sm_count(), kJoinParts / 2);
     const long long heads = p->rows * p->q_heads;
     // Few rows have many pieces each, and leave SMs idle unless several blocks share them; many rows keep every SM busy with 32
-    // rows to a block, which reads each piece's statistics once.  Measured, 8 rows against 32: 56 rows x heads 16.3 us against
-    // 18.9, 448 44.0 against 59.7; 4900 54.6 against 39.7, 6144 147 against 126, 21364 735 against 664.
+    // rows to a block, which reads each piece's statistics once.  Measured, 8 rows against 32: 56 rows x heads 14.9 us against
+    // 17.5, 448 37.7 against 52.1; 4900 52.0 against 36.7, 6144 128 against 112, 21364 709 against 637.
     pl->join_rows = heads <= pl->grid * 32 ? 8 : 32;
     pl->join_grid = (p->rows * group + pl->join_rows - 1) / pl->join_rows * prefix->heads * prefix_join_split(prefix->dim, pl->join_rows);
     if (heads > INT_MAX) return STTM_ERR_UNSUPPORTED;
