@@ -10,8 +10,8 @@
 //
 // Every element is read once and written once, with some ten operations between: HBM bounds it.  A row is held in registers by
 // 32 to 1024 threads; sums of squares run in 32 bits.  Measured: 55724 bf16 rows of 3584, both norms and a gate, 280 us at full
-// clocks (5.7 TB/s, 87 % of the copy rate); quantized 106 us (86 %); 15630 fp16 rows of 1157 with gates of their own 53.5 us
-// (single elements: instructions bound it).
+// clocks (5.7 TB/s, 87 % of the copy rate); quantized 106 us (86 %); 15630 fp16 rows of 1157 with gates of their own 48.8 us
+// (two elements at a time: instructions bound it).
 #pragma once
 
 #include "sttm_cache.cuh"
@@ -74,6 +74,20 @@ struct Elements<float, 4> {
         apart(f[0], w.x, w.y);
         apart(f[1], w.z, w.w);
         *reinterpret_cast<float4*>(p) = w;
+    }
+};
+
+template <typename T>
+struct Elements<T, 2> {
+    typedef uint32_t Raw;
+    static __device__ __forceinline__ void split(const Raw& w, uint64_t (&f)[1]) {
+        const float2 v = Pair<T>::split(w);
+        f[0] = both(v.x, v.y);
+    }
+    static __device__ __forceinline__ void store(T* p, const uint64_t (&f)[1]) {
+        float x, y;
+        apart(f[0], x, y);
+        *reinterpret_cast<uint32_t*>(p) = Pair<T>::pack(x, y);
     }
 };
 
@@ -201,6 +215,28 @@ struct Chunk<T, 1> {
     __device__ __forceinline__ void largest(float& m) const { m = max3(m, fabsf(v), 0.0f); }
     __device__ __forceinline__ void gated(const Chunk& g) { v = v / (1.0f + expf(-v)) * g.v; }
     __device__ __forceinline__ void bytes(int8_t* p, float factor) const { *p = (int8_t)__float2int_rn(v * factor); }
+};
+
+// Two elements of a 16-bit row that share a 32-bit word, parked as Chunk<T, 1> does it.
+template <typename T>
+struct Two : Chunk<T, 2> {
+    __device__ __forceinline__ void kept(const float* p, int i, int) { this->v[0] = both(p[i], p[i + 1]); }
+    __device__ __forceinline__ void park(T* x, T* y) const {
+        float e, f;
+        apart(this->v[0], e, f);
+        *reinterpret_cast<uint32_t*>(x) = __byte_perm(__float_as_uint(e), __float_as_uint(f), 0x5410);
+        *reinterpret_cast<uint32_t*>(y) = __byte_perm(__float_as_uint(e), __float_as_uint(f), 0x7632);
+    }
+    __device__ __forceinline__ void unpark(const T* x, const T* y) {
+        const uint32_t lo = *reinterpret_cast<const uint32_t*>(x), hi = *reinterpret_cast<const uint32_t*>(y);
+        this->v[0] = both(__uint_as_float(__byte_perm(lo, hi, 0x5410)), __uint_as_float(__byte_perm(lo, hi, 0x7632)));
+    }
+    __device__ __forceinline__ void bytes(int8_t* p, float factor) const {
+        float e, f;
+        apart(this->v[0], e, f);
+        p[0] = (int8_t)__float2int_rn(e * factor);
+        p[1] = (int8_t)__float2int_rn(f * factor);
+    }
 };
 
 // Sum of v over the row's threads, and the largest of the bit patterns m (absolute values: their patterns compare as they do,
@@ -391,6 +427,7 @@ struct RowsShape {
 template <typename T, int VEC, bool QUANTIZE>
 __global__ void __launch_bounds__(kRowsWarps * 32) k_norm_rows(const __grid_constant__ NormArgs a, const RowsShape shape) {
     typedef Chunk<T, VEC> C;
+    constexpr bool TWOS = VEC == 1 && sizeof(T) == 2 && !QUANTIZE;
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool second = QUANTIZE ? a.gated : a.residual != nullptr, third = !QUANTIZE && a.gate_rows != nullptr;
@@ -460,17 +497,39 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_norm_rows(const __grid_cons
     for (long long row = first; row < a.rows; row += step) {
         if (!mbar_wait_near(bars + 8 * slot, use, timed_out)) break;
         unsigned char* const at = mine + slot * slot_bytes;
-        auto row_of = [&](int k) { return reinterpret_cast<T*>(at + k * shape.pitch + (VEC == 1 ? (uint32_t)((uintptr_t)source(k, row) & 15) : 0)); };
+        auto row_of = [&](int k) { return reinterpret_cast<T*>(at + k * shape.pitch + (VEC == 1 ? (uint32_t)((uintptr_t)source(k == 1 && !second ? 0 : k, row) & 15) : 0)); };
         T *const xs = row_of(0), *const rs = row_of(1), *const gs = third ? row_of(2) : nullptr;
         float f = 1.0f, s0, s1, m = 0.0f;
         uint64_t squares = 0;
-        if (!QUANTIZE && post != nullptr) {
+        T *const sums = (T*)a.sum + row * a.sum_row, *const outs = (T*)a.out + row * a.out_row;
+        // 16-bit rows of any width go two elements at a time where all arrays' rows begin in the same half of a 32-bit word (15630 rows of
+        // 1157 fp16, gates of their own: 48.8 us, one at a time 53.5)
+        bool twos = false;
+        if constexpr (TWOS) {
+            const uintptr_t x = (uintptr_t)source(0, row);
+            twos = (((second ? x ^ (uintptr_t)source(1, row) : 0) | (third ? x ^ (uintptr_t)source(2, row) : 0) | (a.sum != nullptr ? x ^ (uintptr_t)sums : 0) |
+                     (a.out != nullptr ? x ^ (uintptr_t)outs : 0)) & 2) == 0;
+        }
+        const int begin = TWOS && twos ? (int)((uintptr_t)source(0, row) >> 1 & 1) : 0;
+        auto all = [&](auto&& of) {
+            if constexpr (TWOS) {
+                if (twos) {
+                    const int end = begin + (a.dim - begin) / 2 * 2;
+                    if (lane == 0 && begin > 0) of(C(), 0);
+                    if (lane == 31 && end < a.dim) of(C(), end);
 #pragma unroll 4
-            for (int i = lane * VEC; i < a.dim; i += 32 * VEC) {
-                C r;
-                r.split(*reinterpret_cast<const typename C::Raw*>(xs + i));
-                r.square(squares);
+                    for (int i = begin + lane * 2; i < end; i += 64) of(Two<T>(), i);
+                    return;
+                }
             }
+#pragma unroll 4
+            for (int i = lane * VEC; i < a.dim; i += 32 * VEC) of(C(), i);
+        };
+        if (!QUANTIZE && post != nullptr) {
+            all([&](auto r, int i) {
+                r.split(*reinterpret_cast<const typename decltype(r)::Raw*>(xs + i));
+                r.square(squares);
+            });
             apart(squares, s0, s1);
             s0 += s1;
 #pragma unroll
@@ -478,14 +537,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_norm_rows(const __grid_cons
             f = rsqrtf(s0 * per + a.eps);
             squares = 0;
         }
-        T* const sums = (T*)a.sum + row * a.sum_row;
-#pragma unroll 2
-        for (int i = lane * VEC; i < a.dim; i += 32 * VEC) {
-            C r, w;
-            r.split(*reinterpret_cast<const typename C::Raw*>(xs + i));
+        all([&](auto r, int i) {
+            typedef typename decltype(r)::Raw Raw;
+            decltype(r) w;
+            r.split(*reinterpret_cast<const Raw*>(xs + i));
             if constexpr (QUANTIZE) {
                 if (second) {
-                    w.split(*reinterpret_cast<const typename C::Raw*>(rs + i));
+                    w.split(*reinterpret_cast<const Raw*>(rs + i));
                     r.gated(w);
                 }
             } else {
@@ -499,11 +557,11 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_norm_rows(const __grid_cons
                     r.times(w);
                 }
                 if (third) {
-                    w.split(*reinterpret_cast<const typename C::Raw*>(gs + i));
+                    w.split(*reinterpret_cast<const Raw*>(gs + i));
                     r.times(w);
                 }
                 if (second) {
-                    w.split(*reinterpret_cast<const typename C::Raw*>(rs + i));
+                    w.split(*reinterpret_cast<const Raw*>(rs + i));
                     r.add(a.residual_scale, w);
                 }
                 r.square(squares);
@@ -515,7 +573,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_norm_rows(const __grid_cons
             }
             if (a.q != nullptr) r.largest(m);
             r.park(xs + i, rs + i);
-        }
+        });
         if (a.out != nullptr || a.q != nullptr) {
             apart(squares, s0, s1);
             s0 += s1;
@@ -530,18 +588,15 @@ __global__ void __launch_bounds__(kRowsWarps * 32) k_norm_rows(const __grid_cons
                 quant_step(__reduce_max_sync(0xffffffffu, __float_as_uint(m)), factor, quantum);
                 if (lane == 0) a.q_scale[row] = quantum * f;
             }
-            T* const outs = (T*)a.out + row * a.out_row;
             int8_t* const bytes = a.q + row * a.q_row;
-#pragma unroll 4
-            for (int i = lane * VEC; i < a.dim; i += 32 * VEC) {
-                C r;
+            all([&](auto r, int i) {
                 r.unpark(xs + i, rs + i);
                 if (a.q != nullptr) r.bytes(bytes + i, factor);
                 if (!QUANTIZE && a.out != nullptr) {
                     r.scale(f);
                     r.store(outs + i);
                 }
-            }
+            });
         }
         __syncwarp();
         load(row + shape.slots * step, slot);

@@ -22,7 +22,7 @@ sttm_status by_element(int dtype, F&& f) {
 }
 
 // Many rows: a warp each out of shared memory, where that holds six or more and every warp gets four or more (55724 rows of 3584 bf16, both norms and a
-// gate: 280 us against 305 in blocks; 15630 of 1157 fp16 with gates of their own 54 against 92; but 5278 rows, 2.4 a warp, 35 against 28).
+// gate: 280 us against 305 in blocks; 15630 of 1157 fp16 with gates of their own 49 against 92; but 5278 rows, 2.4 a warp, 35 against 28).
 // Else a block each: short rows a warp, few rows the fewest threads that hold one with one chunk (of 16 bytes, or of one element where rows do not
 // fill whole 16-byte words) each, two of fp32, eight single elements (one row of 3584: 4.1 us on its own, with four chunks a thread 5.9); more rows
 // than the GPU takes at once four chunks a thread (5278 rows: 28 us, with one 35).
