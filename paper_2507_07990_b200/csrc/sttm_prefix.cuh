@@ -785,6 +785,9 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tmem_wait_store();
                 tc_fence_before();
                 __syncwarp();
+                // With two places for one block's logits the product before may still run: it is waited for here, since a wait for this
+                // tile's, by its parity, would take that of two tiles before for it.
+                if (SETS == 1 && o_uses > 0 && !mbar_wait_near(o_full + 8 * set, o_uses - 1, timed_out)) break;
                 if (lane == 0) mbar_arrive(p_full + 8 * b);
                 o_uses++;
             }

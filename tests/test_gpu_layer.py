@@ -120,6 +120,18 @@ def test_many_rows(dtype, width, stride, shift):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width,starts", [(1157, (0, 1, 0)), (1157, (1, 1, 1)), (334, (1, 1, 0)), (65, (1, 0, 1))])
+def test_many_rows_that_begin_in_different_halves_of_a_word(dtype, width, starts):
+    gen = torch.Generator().manual_seed(width + starts[1])
+    rows = 1301
+    w = [(1 + 0.3 * torch.randn(width, generator=gen)).cuda() for _ in range(2)]
+    x, residual, gate = (rows_of(gen, rows, width, dtype, width + (i & 1), s) for i, s in enumerate(starts))
+    for quantize in (False, True):
+        got = layer.NormPlan(width, dtype, rows, eps=1e-5, post_norm=w[0], pre_norm=w[1], residual_scale=0.7, quantize=quantize).run(x, residual, gate=gate)
+        check_norm(got, x, residual, w[0], [gate], 0.7, w[1], 1e-5, quantize)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,width", [(1, 14336), (33, 64), (5, 1157), (4, 3584), (3, 1), (2, 16384)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_quantize_rows(dtype, rows, width, gated):

@@ -179,6 +179,15 @@ def test_more_sequences_than_threads():
     check(p, run(p))
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("f16", 256)])
+def test_many_pieces_of_every_kind_to_a_block(dtype, dim):
+    # own slots of one tile, of several, of none, and new tokens of more than one block of rows, by turns
+    n = 120
+    new, held = [(1, 2, 40, 0)[b % 4] for b in range(n)], [(5, 150, 0, 0, 260)[b % 5] for b in range(n)]
+    p = problem(21, dtype=dtype, dim=dim, q_heads=32, heads=8, page=16, lens=(130, 700), groups=(50, 70), new=new, held=held)
+    check(p, run(p))
+
+
 def test_hidden_values_do_not_matter_but_seen_ones_do():
     p = problem(9, lens=(100,), groups=(2,), new=(2, 2), held=(0, 0))
     p["mine"][1][int(p["mine"][2][0, 0]), :, 0] = math.nan      # sequence 0's first slot: seen by its tokens
