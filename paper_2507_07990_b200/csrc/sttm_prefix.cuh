@@ -808,7 +808,8 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     const float most = fmaxf(m, other.x);
                     f0 = m == -INFINITY ? 0.0f : exp2_fast((m - most) * a.scale_log2);
                     f1 = other.x == -INFINITY ? 0.0f : exp2_fast((other.x - most) * a.scale_log2);
-                    l = (m == -INFINITY ? 0.0f : f0 * l) + (other.x == -INFINITY ? 0.0f : f1 * other.y);
+                    // (without a maximum l is 0, or NaN: logits that are all NaN have none, and have to reach the output)
+                    l = (m == -INFINITY ? l : f0 * l) + (other.x == -INFINITY ? other.y : f1 * other.y);
                     m = most;
                     stat[row] = make_float2(f0, f1);
                 }
