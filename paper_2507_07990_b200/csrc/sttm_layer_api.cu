@@ -154,11 +154,15 @@ sttm_status launch_matmul(const MatmulArgs& a, const MatmulPlan& pl, const CUten
 bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
     return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
 }
-// Do two arrays of `rows` rows share memory, other than one in the other's place?
-bool clash(const void* out, long long out_row, const void* in, long long in_row, long long rows, long long width) {
-    if (out == nullptr || in == nullptr || (out == in && (out_row == in_row || rows == 1))) return false;
-    return overlap(out, (rows - 1) * out_row + width, in, (rows - 1) * in_row + width);
+// `rows` rows of `width` bytes, `row` bytes apart
+struct RowsAt {
+    const void* at;
+    long long row, width;
+};
+bool share_memory(const RowsAt& a, const RowsAt& b, long long rows) {
+    return a.at != nullptr && b.at != nullptr && overlap(a.at, (rows - 1) * a.row + a.width, b.at, (rows - 1) * b.row + b.width);
 }
+bool in_place(const RowsAt& a, const RowsAt& b, long long rows) { return a.at == b.at && a.width == b.width && (a.row == b.row || rows == 1); }
 
 }  // namespace
 
@@ -187,12 +191,13 @@ sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream) {
     const uintptr_t weights = (uintptr_t)p->post_norm | (uintptr_t)p->gate | (uintptr_t)p->pre_norm;
     wide = wide && weights % 16 == 0 && (p->q == nullptr || (!misaligned(p->q, 8) && (p->rows == 1 || p->q_row % 8 == 0)));
     for (int o = 0; o < 3; o++) {
-        const long long ob = o < 2 ? out_row[o] * e : out_row[o], ow = o < 2 ? width : p->dim;
-        for (int i = 0; i < 3; i++)
-            if (o < 2 ? clash(out[o], ob, in[i], in_row[i] * e, p->rows, width)
-                      : out[o] && in[i] && (out[o] == in[i] || clash(out[o], ob, in[i], in_row[i] * e, p->rows, width))) return STTM_ERR_ARG;
+        const RowsAt to = o < 2 ? RowsAt{out[o], out_row[o] * e, width} : RowsAt{p->q, p->q_row, p->dim};
+        for (int i = 0; i < 3; i++) {
+            const RowsAt from = {in[i], in_row[i] * e, width};
+            if (share_memory(to, from, p->rows) && !in_place(to, from, p->rows)) return STTM_ERR_ARG;
+        }
         for (int u = 0; u < o; u++)
-            if (out[o] && out[u] && (out[o] == out[u] || clash(out[o], ob, out[u], out_row[u] * e, p->rows, std::max(ow, width)))) return STTM_ERR_ARG;
+            if (share_memory(to, {out[u], out_row[u] * e, width}, p->rows)) return STTM_ERR_ARG;
     }
     NormArgs a = {};
     a.x = p->x; a.residual = p->residual; a.gate_rows = p->gate_rows;
@@ -220,7 +225,7 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream) {
     const long long e = p->dtype == STTM_F32 ? 4 : 2, in = p->gated ? 2ll * p->dim : p->dim;
     if (misaligned(p->x, e) || (p->rows > 1 && (p->x_row < in || p->q_row < p->dim || p->x_row > LLONG_MAX / 4 / p->rows || p->q_row > LLONG_MAX / 4 / p->rows)))
         return STTM_ERR_ARG;
-    if ((const void*)p->q == p->x || clash(p->q, p->q_row, p->x, p->x_row * e, p->rows, in * e)) return STTM_ERR_ARG;
+    if (share_memory({p->q, p->q_row, p->dim}, {p->x, p->x_row * e, in * e}, p->rows)) return STTM_ERR_ARG;
     const bool wide = p->dim % (16 / e) == 0 && !misaligned(p->x, 16) && !misaligned(p->q, 8) && (p->rows == 1 || (p->x_row * e % 16 == 0 && p->q_row % 8 == 0));
     NormArgs a = {};
     a.x = p->x; a.x_row = p->x_row;
