@@ -440,7 +440,8 @@ typedef struct sttm_prefix_params {
     int max_prefix, max_own;      /* no length is larger (else it is cut and 1 << STTM_ERR_CAPACITY raised); at most what the
                                      tables have room for, and below 2^31 - 2^20                   */
     float scale;                  /* above 0                                                       */
-    void* out;                    /* [rows][q_heads][dim] contiguous, 16-byte aligned              */
+    void* out;                    /* [rows][q_heads][dim] contiguous, 16-byte aligned; may lie where q does, and shares
+                                     no memory with the other arrays                               */
     float* lse;                   /* [rows][q_heads] log of the sum of exp(scale q . k), may be NULL */
     int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_CAPACITY (also: offsets beyond the rows), 1 << STTM_ERR_ARG
                                      (a page that is not there: read as zeros; offsets that decrease: nothing is written),
@@ -459,8 +460,8 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
  * with N(y; w) = y / sqrt(mean y^2 + eps) * w, or y itself where w is NULL.  All but x may be left out: no residual is 0, no
  * gate 1; gate and gate_rows both count where both are given.  `out` is normed from r before it is rounded to `sum`.  q and
  * q_scale hold `out` in 8 bits (see sttm_quantize_rows).  Outputs may take the place of inputs row by row (same address and
- * row stride); otherwise the memory from an output's first row to its last and that of any other array do not overlap.  Squares are
- * summed in 32 bits.
+ * row stride); otherwise the memory from an output's first row to its last and that of any other array do not overlap (such calls
+ * are refused, here and below).  Squares are summed in 32 bits.
  */
 typedef struct sttm_norm_params {
     const void* x;                /* [rows][dim] the block's output                                */
@@ -504,7 +505,7 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream);
 /*
  * Matrix product of 8-bit rows: out[t][n] = x_scale[t] * w_scale[n] * (sum over k of x[t][k] * w[n][k]) + bias[n], the sums
  * exact, one rounding to out's type.  Both operands are [rows][inner] with 16-byte aligned rows; what lies between inner
- * and the row's end does not matter.  The memory from out's first row to its last and that of either operand do not overlap.  Weights are quantized once, by sttm_quantize_rows over their output channels.
+ * and the row's end does not matter.  The memory from out's first row to its last and that of any other array do not overlap.  Weights are quantized once, by sttm_quantize_rows over their output channels.
  */
 typedef struct sttm_matmul_params {
     const int8_t* x;              /* [rows][inner] tokens, 16-byte aligned                         */

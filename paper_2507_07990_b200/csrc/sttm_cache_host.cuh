@@ -51,6 +51,17 @@ inline bool multiple_of_8(long long v) { return v % 8 == 0; }
 template <typename... P>
 inline bool odd_address(const P*... p) { return (((uintptr_t)p | ...) & 3) != 0; }
 
+struct Span {
+    const void* at;               // or NULL: nothing
+    long long bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+    return a.at != nullptr && b.at != nullptr && (uintptr_t)a.at < (uintptr_t)b.at + (uintptr_t)b.bytes && (uintptr_t)b.at < (uintptr_t)a.at + (uintptr_t)a.bytes;
+}
+// does `a` share memory with any of these?
+template <typename... S>
+bool overlaps_any(const Span& a, const S&... others) { return (overlap(a, others) || ...); }
+
 inline sttm_status check_cache(const sttm_cache* c) {
     if (c == nullptr || c->k == nullptr || c->v == nullptr || c->table == nullptr) return STTM_ERR_ARG;
     if (c->pages < 1 || c->heads < 1 || c->page < 1 || c->seqs < 1 || c->table_width < 1 || c->dim < 1) return STTM_ERR_ARG;

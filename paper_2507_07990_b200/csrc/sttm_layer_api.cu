@@ -151,17 +151,13 @@ sttm_status launch_matmul(const MatmulArgs& a, const MatmulPlan& pl, const CUten
     return s != STTM_OK ? s : launch(k_quant_matmul<T, NT>, pl.grid, kMatThreads, smem, pl.cluster > 1 ? pl.cluster : 0, stream, a, ma, mb);
 }
 
-bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
-    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
-}
 // `rows` rows of `width` bytes, `row` bytes apart
 struct RowsAt {
     const void* at;
     long long row, width;
 };
-bool share_memory(const RowsAt& a, const RowsAt& b, long long rows) {
-    return a.at != nullptr && b.at != nullptr && overlap(a.at, (rows - 1) * a.row + a.width, b.at, (rows - 1) * b.row + b.width);
-}
+Span span_of(const RowsAt& a, long long rows) { return {a.at, (rows - 1) * a.row + a.width}; }
+bool share_memory(const RowsAt& a, const RowsAt& b, long long rows) { return overlap(span_of(a, rows), span_of(b, rows)); }
 bool in_place(const RowsAt& a, const RowsAt& b, long long rows) { return a.at == b.at && a.width == b.width && (a.row == b.row || rows == 1); }
 
 }  // namespace
@@ -190,11 +186,15 @@ sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream) {
     if (odd_address(p->post_norm, p->gate, p->pre_norm, p->q_scale, p->device_status)) return STTM_ERR_ARG;
     const uintptr_t weights = (uintptr_t)p->post_norm | (uintptr_t)p->gate | (uintptr_t)p->pre_norm;
     wide = wide && weights % 16 == 0 && (p->q == nullptr || (!misaligned(p->q, 8) && (p->rows == 1 || p->q_row % 8 == 0)));
+    const Span post = {p->post_norm, p->dim * 4ll}, gate = {p->gate, p->dim * 4ll}, pre = {p->pre_norm, p->dim * 4ll};
+    const Span scales = {p->q_scale, p->rows * 4}, status = {p->device_status, 4};
+    if (overlaps_any(scales, post, gate, pre, status)) return STTM_ERR_ARG;
     for (int o = 0; o < 3; o++) {
         const RowsAt to = o < 2 ? RowsAt{out[o], out_row[o] * e, width} : RowsAt{p->q, p->q_row, p->dim};
+        if (overlaps_any(span_of(to, p->rows), post, gate, pre, scales, status)) return STTM_ERR_ARG;
         for (int i = 0; i < 3; i++) {
             const RowsAt from = {in[i], in_row[i] * e, width};
-            if (share_memory(to, from, p->rows) && !in_place(to, from, p->rows)) return STTM_ERR_ARG;
+            if ((share_memory(to, from, p->rows) && !in_place(to, from, p->rows)) || overlap(scales, span_of(from, p->rows))) return STTM_ERR_ARG;
         }
         for (int u = 0; u < o; u++)
             if (share_memory(to, {out[u], out_row[u] * e, width}, p->rows)) return STTM_ERR_ARG;
@@ -225,7 +225,8 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream) {
     const long long e = p->dtype == STTM_F32 ? 4 : 2, in = p->gated ? 2ll * p->dim : p->dim;
     if (misaligned(p->x, e) || (p->rows > 1 && (p->x_row < in || p->q_row < p->dim || p->x_row > LLONG_MAX / 4 / p->rows || p->q_row > LLONG_MAX / 4 / p->rows)))
         return STTM_ERR_ARG;
-    if (share_memory({p->q, p->q_row, p->dim}, {p->x, p->x_row * e, in * e}, p->rows)) return STTM_ERR_ARG;
+    const Span x = span_of({p->x, p->x_row * e, in * e}, p->rows), q = span_of({p->q, p->q_row, p->dim}, p->rows), scales = {p->scale, p->rows * 4};
+    if (overlaps_any(q, x, scales, Span{p->device_status, 4}) || overlaps_any(scales, x, Span{p->device_status, 4})) return STTM_ERR_ARG;
     const bool wide = p->dim % (16 / e) == 0 && !misaligned(p->x, 16) && !misaligned(p->q, 8) && (p->rows == 1 || (p->x_row * e % 16 == 0 && p->q_row % 8 == 0));
     NormArgs a = {};
     a.x = p->x; a.x_row = p->x_row;
@@ -243,14 +244,19 @@ sttm_status sttm_quantize_rows(const sttm_quantize_params* p, void* stream) {
 sttm_status sttm_quant_matmul(const sttm_matmul_params* p, void* stream) {
     if (p == nullptr || p->rows < 0 || p->inner < 1 || p->outer < 1 || !known_type(p->out_dtype)) return STTM_ERR_ARG;
     if (p->inner > 131056 || p->rows > INT_MAX) return STTM_ERR_UNSUPPORTED;
-    if (p->w == nullptr || p->w_scale == nullptr || misaligned(p->w, 16) || p->w_row % 16 != 0 || p->w_row < p->inner) return STTM_ERR_ARG;
+    if (p->w == nullptr || p->w_scale == nullptr || misaligned(p->w, 16) || p->w_row % 16 != 0 || p->w_row < p->inner || p->w_row > LLONG_MAX / 4 / p->outer)
+        return STTM_ERR_ARG;
     if (odd_address(p->x_scale, p->w_scale, p->bias, p->device_status)) return STTM_ERR_ARG;
     if (p->rows == 0) return STTM_OK;
-    if (p->x == nullptr || p->x_scale == nullptr || p->out == nullptr || misaligned(p->x, 16) || p->x_row % 16 != 0 || p->x_row < p->inner) return STTM_ERR_ARG;
+    if (p->x == nullptr || p->x_scale == nullptr || p->out == nullptr || misaligned(p->x, 16) || p->x_row % 16 != 0 || p->x_row < p->inner ||
+        p->x_row > LLONG_MAX / 4 / p->rows)
+        return STTM_ERR_ARG;
     const int e = p->out_dtype == STTM_F32 ? 4 : 2;
     if (misaligned(p->out, e) || (p->rows > 1 && (p->out_row < p->outer || p->out_row > LLONG_MAX / 4 / p->rows))) return STTM_ERR_ARG;
-    const long long span = (p->rows - 1) * (p->rows > 1 ? p->out_row : 0) * e + (long long)p->outer * e;
-    if (overlap(p->out, span, p->x, (p->rows - 1) * p->x_row + p->inner) || overlap(p->out, span, p->w, (p->outer - 1ll) * p->w_row + p->inner)) return STTM_ERR_ARG;
+    if (overlaps_any(span_of({p->out, p->out_row * e, (long long)p->outer * e}, p->rows), span_of({p->x, p->x_row, p->inner}, p->rows),
+                     span_of({p->w, p->w_row, p->inner}, p->outer), Span{p->x_scale, p->rows * 4}, Span{p->w_scale, p->outer * 4ll},
+                     Span{p->bias, p->outer * 4ll}, Span{p->device_status, 4}))
+        return STTM_ERR_ARG;
     const MatmulPlan pl = plan_matmul(p);
     if (pl.a_tiles * pl.b_tiles > INT_MAX / 8) return STTM_ERR_UNSUPPORTED;
     MatmulArgs a = {};

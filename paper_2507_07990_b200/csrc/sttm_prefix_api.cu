@@ -98,12 +98,21 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
     if (!std::isfinite(p->scale) || !(p->scale > 0.0f)) return STTM_ERR_ARG;
     if (p->rows > 0) {
         if (p->q == nullptr || p->out == nullptr || misaligned(p->q, 16) || misaligned(p->out, 16)) return STTM_ERR_ARG;
-        if ((p->rows > 1 && (!multiple_of_8(p->q_row) || p->q_row < prefix->dim)) ||
-            (p->q_heads > 1 && (!multiple_of_8(p->q_head) || p->q_head < prefix->dim)))
+        if ((p->rows > 1 && (!multiple_of_8(p->q_row) || p->q_row < prefix->dim || p->q_row > LLONG_MAX / 8 / p->rows)) ||
+            (p->q_heads > 1 && (!multiple_of_8(p->q_head) || p->q_head < prefix->dim || p->q_head > LLONG_MAX / 8 / p->q_heads)))
             return STTM_ERR_ARG;
     }
     if (ws_bytes < pl.total) return STTM_ERR_WORKSPACE;
     if (p->rows == 0) return STTM_OK;
+    // (out may lie where q does: the first kernel has read it by then)
+    const long long heads = p->rows * p->q_heads;
+    const Span out = {p->out, heads * prefix->dim * 2}, lse = {p->lse, heads * 4}, space = {ws, (long long)pl.total}, status = {p->device_status, 4};
+    const Span q = {p->q, ((p->rows > 1 ? (p->rows - 1) * p->q_row : 0) + (p->q_heads > 1 ? (p->q_heads - 1) * p->q_head : 0) + prefix->dim) * 2};
+    const Span offsets = {p->row_offsets, (p->seqs + 1ll) * 8}, seq_offsets = {p->seq_offsets, (prefix->seqs + 1ll) * 4};
+    const Span shared = {p->prefix_lengths, prefix->seqs * 4ll}, own_slots = {own != nullptr ? p->lengths : nullptr, p->seqs * 4ll};
+    if (overlaps_any(out, lse, offsets, seq_offsets, shared, own_slots, status) || overlaps_any(lse, offsets, seq_offsets, shared, own_slots, status) ||
+        overlaps_any(space, out, lse, q, offsets, seq_offsets, shared, own_slots, status))
+        return STTM_ERR_ARG;
     char* w = (char*)ws;
     PrefixArgs a = {};
     a.prefix = view_of(prefix);

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2507_07990_b200 import binding, layer
+from tests.test_gpu_prefix import plan_of, problem, run
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +83,30 @@ def test_a_norms_8_bit_rows_beside_its_other_arrays(q_first, beside, rows, dim, 
         assert torch.equal(got, w)
     closer = q.data_ptr() + gap + 1 if q_first else q.data_ptr() - 1
     assert call("sttm_block_norm", layer.NormParams, q=closer, **arrays, **args) == ARG
+
+
+@pytest.mark.parametrize("rows", [1, 40, 500])
+def test_a_products_arrays_beside_each_other(rows):
+    gen = torch.Generator().manual_seed(rows)
+    x, w = (layer.sttm_quantize_rows(torch.randn((n, 1024), generator=gen).cuda()) for n in (rows, 336))
+    bias = torch.randn(336, generator=gen).cuda()
+    want = layer.sttm_quant_matmul(x, w, torch.bfloat16, bias)
+    flat = torch.zeros(rows * (1024 + 4 + 672) + 336 * (1024 + 8) + 256, dtype=torch.int8, device="cuda")
+    for order in (["out", "x", "w", "x_scale", "w_scale", "bias"], ["x", "out", "w_scale", "bias", "w", "x_scale"]):
+        at, placed = 0, {}
+        for name in order:
+            data = dict(x=x.q, w=w.q, x_scale=x.scale.unsqueeze(1), w_scale=w.scale.unsqueeze(1), bias=bias.unsqueeze(1), out=torch.zeros_like(want))[name]
+            at = -(-at // 16) * 16
+            placed[name], at = cut(flat, at, data.shape[0], data.shape[1], data.dtype)
+            placed[name].copy_(data)
+        assert call("sttm_quant_matmul", layer.MatmulParams, x_row=1024, w_row=1024, rows=rows, inner=1024, outer=336, out_row=336, out_dtype=0, **placed) == 0
+        assert torch.equal(placed["out"], want)
+
+
+@pytest.mark.parametrize("length,new", [(300, (1, 2)), (3000, (70, 41))])
+def test_attention_written_where_the_queries_lie(length, new):
+    p = problem(3, q_heads=8, heads=2, lens=(length,), groups=(2,), new=new, held=(3, 0), spare=0)
+    p["q"] = p["q"].contiguous()
+    plan = plan_of(p)
+    want = run(p, plan).out.clone()
+    assert torch.equal(run(p, plan, out=p["q"]).out, want) and torch.equal(p["q"], want)
