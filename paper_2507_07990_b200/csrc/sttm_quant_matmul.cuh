@@ -76,8 +76,10 @@ __device__ __forceinline__ void tile_at(const MatmulArgs& a, int tile, int& ta, 
     ta = first + in - tb * size;
 }
 
+// A sum as an output.  (The fused form by name: left to the compiler, one of the places below had two roundings where the others have one, and a token's
+// last bits in 32-bit outputs depended on how many others came with it.)
 template <typename T>
-__device__ __forceinline__ T narrow(float v) { return (T)v; }
+__device__ __forceinline__ T output(int sum, float xs, float ws, float bias) { return (T)fmaf((float)sum * xs, ws, bias); }
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_constant__ MatmulArgs a, const __grid_constant__ CUtensorMap map_a,
@@ -200,7 +202,7 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
                 const float ws = ch < a.outer ? a.w_scale[ch] : 0.0f, bias = a.bias && ch < a.outer ? a.bias[ch] : 0.0f;
                 auto write = [&](int col, int sum) {
                     const long long token = (long long)tb * NT + col;
-                    if (ch < a.outer && token < a.rows) ((T*)a.out)[token * a.out_row + ch] = narrow<T>((float)sum * a.x_scale[token] * ws + bias);
+                    if (ch < a.outer && token < a.rows) ((T*)a.out)[token * a.out_row + ch] = output<T>(sum, a.x_scale[token], ws, bias);
                 };
                 constexpr int CH = NT < 32 ? NT : 32;
 #pragma unroll 1
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
                         T* const out = (T*)a.out + token * a.out_row + ch0;
 #pragma unroll
                         for (int i = 0; i < 4; i++)
-                            if (ch0 + i < a.outer) out[i] = narrow<T>((float)sum[i] * xs * scale[i] + add[i]);
+                            if (ch0 + i < a.outer) out[i] = output<T>(sum[i], xs, scale[i], add[i]);
                     }
                 }
             }
@@ -427,10 +429,10 @@ k_quant_matmul_pair(const __grid_constant__ MatmulArgs a, const __grid_constant_
                         for (int j = 0; j < PER; j += 4) {
                             const float4 w = __ldg(reinterpret_cast<const float4*>(a.w_scale + ch0 + i + j));
                             const float4 o = a.bias ? __ldg(reinterpret_cast<const float4*>(a.bias + ch0 + i + j)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            piece[j] = narrow<T>((float)(int)v[i + j] * xs * w.x + o.x);
-                            piece[j + 1] = narrow<T>((float)(int)v[i + j + 1] * xs * w.y + o.y);
-                            piece[j + 2] = narrow<T>((float)(int)v[i + j + 2] * xs * w.z + o.z);
-                            piece[j + 3] = narrow<T>((float)(int)v[i + j + 3] * xs * w.w + o.w);
+                            piece[j] = output<T>((int)v[i + j], xs, w.x, o.x);
+                            piece[j + 1] = output<T>((int)v[i + j + 1], xs, w.y, o.y);
+                            piece[j + 2] = output<T>((int)v[i + j + 2], xs, w.z, o.z);
+                            piece[j + 3] = output<T>((int)v[i + j + 3], xs, w.w, o.w);
                         }
                         *reinterpret_cast<uint4*>(out + ch0 + i) = *reinterpret_cast<const uint4*>(piece);
                     }
@@ -438,7 +440,7 @@ k_quant_matmul_pair(const __grid_constant__ MatmulArgs a, const __grid_constant_
 #pragma unroll
                     for (int i = 0; i < 32; i++) {
                         const int ch = ch0 + i;
-                        if (ch < a.outer) out[ch] = narrow<T>((float)(int)v[i] * xs * a.w_scale[ch] + (a.bias ? a.bias[ch] : 0.0f));
+                        if (ch < a.outer) out[ch] = output<T>((int)v[i], xs, a.w_scale[ch], a.bias ? a.bias[ch] : 0.0f);
                     }
                 }
             }
