@@ -777,6 +777,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(p_half + 8 * b);
+                        __syncwarp();
                     }
                 }
                 float s0, s1;
@@ -829,6 +830,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
 #pragma unroll
                     for (int k = 0; k < 32; k++) o[k] = __float_as_uint(f0 * __uint_as_float(o[k]) + f1 * __uint_as_float(u[k]));
                     if (there) store32(to + (i / 4) * rows, rows, o);
+                    __syncwarp();                               // (the next load is one for the whole warp)
                 }
                 tc_fence_before();
                 named_sync(1, 256);                             // before either set's O is begun again
@@ -838,6 +840,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                     uint32_t o[32];
                     tc_load32(o_at + i, o);
                     if (there) store32(to + (i / 4) * rows, rows, o);
+                    __syncwarp();
                 }
                 tc_fence_before();
             }

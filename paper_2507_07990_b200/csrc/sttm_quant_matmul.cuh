@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(kMatThreads) k_quant_matmul(const __grid_const
 #pragma unroll
                         for (int i = 0; i < CH; i++) write(c + i, (int)v[i]);
                     }
+                    __syncwarp();                               // (the next load is one for the whole warp)
                 }
                 if (size > 1) {                                 // (one tile per cluster then, and the ring has been read)
                     cluster_arrive();
@@ -419,8 +420,9 @@ k_quant_matmul_pair(const __grid_constant__ MatmulArgs a, const __grid_constant_
                 uint32_t v[32];
                 tc_load32(mine + b * 256 + c, v);
                 const int ch0 = tb * 256 + c;
-                if (token >= a.rows) continue;
-                if (a.wide && weights_wide && ch0 + 32 <= a.outer) {
+                if (token >= a.rows) {
+                    // nothing to write
+                } else if (a.wide && weights_wide && ch0 + 32 <= a.outer) {
                     constexpr int PER = 16 / sizeof(T);
 #pragma unroll
                     for (int i = 0; i < 32; i += PER) {
@@ -443,6 +445,7 @@ k_quant_matmul_pair(const __grid_constant__ MatmulArgs a, const __grid_constant_
                         if (ch < a.outer) out[ch] = output<T>((int)v[i], xs, a.w_scale[ch], a.bias ? a.bias[ch] : 0.0f);
                     }
                 }
+                __syncwarp();                                   // (the next load is one for the whole warp, and some lanes may have no token)
             }
             tc_fence_before();
             __syncwarp();
