@@ -434,10 +434,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 start->at = e;
             }
             if (blockIdx.x == 0 && e < entries) a.entries[e] = x;
-            // the tokens' entries, shared between the CTAs (one does it where entries are so many that the others do not see them all)
-            if (e < entries && x.units > 0 && (once || blockIdx.x == 0))
-                for (int i = once ? blockIdx.x : 0; i < x.tokens; i += once ? gridDim.x : 1) (e < a.prefix.seqs ? a.prefix_of : a.own_of)[x.first + i] = e;
-            if (blockIdx.x != 0 && !once && steps > walk.step) break;       // (the same for the whole CTA)
+            // The tokens' entries, shared between the CTAs, all of which go through all entries for it.  (One CTA's thread per entry instead, with the
+            // others stopping at their first step: 390 questions of 50 tokens 442 us against 96, 3200 of one token 208 against 148.)
+            if (e < entries && x.units > 0)
+                for (long long i = blockIdx.x; i < x.tokens; i += gridDim.x) (e < a.prefix.seqs ? a.prefix_of : a.own_of)[x.first + i] = e;
         }
     }
     __syncthreads();
