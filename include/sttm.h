@@ -492,7 +492,8 @@ typedef struct sttm_quantize_params {
     const void* x;
     long long x_row;              /* stride in elements, at least dim (gated: 2 dim)               */
     long long rows;
-    int dim;                      /* at most 16384                                                 */
+    int dim;                      /* at most 16384, or 32768 where the rows of x (and both halves of gated ones) begin and end
+                                     on 16 bytes and those of q on 8                               */
     int dtype;                    /* of x                                                          */
     int gated;
     int8_t* q;                    /* [rows][dim] out                                               */

@@ -34,7 +34,7 @@ struct NormArgs {
     int32_t* status;
 };
 
-constexpr int kNormMaxDim = 16384;
+constexpr int kNormMaxDim = 16384, kQuantizeMaxDim = 32768;     // (beyond the first: rows of whole 16-byte words only)
 
 // VEC elements in 16 bytes, or one.  A row's words are all on their way before the first is used, and before anything is stored: an
 // output may take the place of an input, so the compiler moves no load over a store (plain loads, for the same reason).

@@ -145,7 +145,8 @@ class NormPlan:
 
 
 class QuantizePlan:
-    """Repeated sttm_quantize_rows calls.  ``gated``: rows are ``[a | b]`` of ``2 dim`` channels and ``silu(a) * b`` is quantized."""
+    """Repeated sttm_quantize_rows calls.  ``gated``: rows are ``[a | b]`` of ``2 dim`` channels and ``silu(a) * b`` is quantized.  More than
+    16384 channels, up to 32768, want rows of whole 16-byte words."""
 
     def __init__(self, dim: int, dtype: torch.dtype, max_rows: int, gated: bool = False, device="cuda"):
         _want(dtype in _TYPES and dim >= 1 and max_rows >= 0, "rows must be bf16, fp16 or fp32, of at least one channel")
