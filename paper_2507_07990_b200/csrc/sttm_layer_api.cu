@@ -170,10 +170,9 @@ extern "C" {
 sttm_status sttm_block_norm(const sttm_norm_params* p, void* stream) {
     if (p == nullptr || p->rows < 0 || p->dim < 1 || !known_type(p->dtype)) return STTM_ERR_ARG;
     if (p->dim > kNormMaxDim || p->rows > INT_MAX) return STTM_ERR_UNSUPPORTED;
-    if (p->sum == nullptr && p->out == nullptr && p->q == nullptr) return STTM_ERR_ARG;
-    if ((p->q == nullptr) != (p->q_scale == nullptr) || !std::isfinite(p->residual_scale) || !(p->eps >= 0.0f)) return STTM_ERR_ARG;
+    if (!std::isfinite(p->residual_scale) || !(p->eps >= 0.0f)) return STTM_ERR_ARG;
     if (p->rows == 0) return STTM_OK;
-    if (p->x == nullptr) return STTM_ERR_ARG;
+    if (p->x == nullptr || (p->sum == nullptr && p->out == nullptr && p->q == nullptr) || (p->q == nullptr) != (p->q_scale == nullptr)) return STTM_ERR_ARG;
     const long long e = p->dtype == STTM_F32 ? 4 : 2, width = p->dim * e;
     const void* const in[3] = {p->x, p->residual, p->gate_rows};
     const long long in_row[3] = {p->x_row, p->residual_row, p->gate_row};
