@@ -81,8 +81,8 @@ int matmul_clusters(int size) {
     static int cached[kMaxDevices][9] = {};
     const int dev = device_slot();
     if (dev < 0) return sm_count() * 2 / size;
-    int& n = cached[dev][size];
-    if (n == 0) {
+    int n = cached[dev][size];
+    if (n == 0) {                                               // (two threads at once find the same)
         const auto kernel = k_quant_matmul<__nv_bfloat16, 16>;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)size);
@@ -95,8 +95,11 @@ int matmul_clusters(int size) {
         cfg.attrs = &at;
         cfg.numAttrs = 1;
         static size_t allowed[kMaxDevices] = {};
-        if (allow_smem((const void*)kernel, kMatSmem, allowed) != STTM_OK || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1)
+        if (allow_smem((const void*)kernel, kMatSmem, allowed) != STTM_OK || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+            (void)cudaGetLastError();                           // (not for the next call on this thread to find)
             n = sm_count() * 2 / size;
+        }
+        cached[dev][size] = n;
     }
     return n;
 }
