@@ -21,8 +21,10 @@ sttm_status by_element(int dtype, F&& f) {
     return dtype == STTM_BF16 ? f(__nv_bfloat16()) : dtype == STTM_F16 ? f(__half()) : f(0.0f);
 }
 
-// Many rows: a warp each out of shared memory, where that holds six or more and every warp gets four or more (55724 rows of 3584 bf16, both norms and a
-// gate: 280 us against 305 in blocks; 15630 of 1157 fp16 with gates of their own 49 against 92; but 5278 rows, 2.4 a warp, 35 against 28).
+// Many rows: a warp each out of shared memory, where that holds six or more and there are four or more to each of the rows that a warp has on its way (1 to 4
+// slots).  One slot: 55724 rows of 3584 bf16, both norms and a gate, 280 us against 305 in blocks; 15630 of 1157 fp16 with gates of their own 49 against
+// 92; but 5278 rows of 3584, 2.4 a warp, 35 against 28.  Four slots (both norms, L2 cold): 56832 rows of 256 bf16, 16 a warp, 37 against 43, 28416 22.5 against
+// 26; below the rule the two are even (14208 rows of 512, 4 a warp, 20.5 both; 7104 14.3 both).
 // Else a block each: short rows a warp, few rows the fewest threads that hold one with one chunk (of 16 bytes, or of one element where rows do not
 // fill whole 16-byte words) each, two of fp32, eight single elements (one row of 3584: 4.1 us on its own, with four chunks a thread 5.9); more rows
 // than the GPU takes at once four chunks a thread (5278 rows: 28 us, with one 35).
