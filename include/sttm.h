@@ -446,6 +446,9 @@ typedef struct sttm_prefix_params {
     int32_t* device_status;       /* may be NULL; OR-ed with 1 << STTM_ERR_CAPACITY (also: offsets beyond the rows), 1 << STTM_ERR_ARG
                                      (a page that is not there: read as zeros; offsets that decrease: nothing is written),
                                      1 << STTM_ERR_TIMEOUT */
+    int fine;                     /* 0: weights are rounded to the cache's type before they meet the values, half a step as for the
+                                     output; else they keep 16 bits (22 in fp16), as in sttm_cache_attend: closer by a factor
+                                     of 1.4, 4 to 30 percent slower                                */
 } sttm_prefix_params;
 /* Workspace of a call: depends on rows, seqs, q_heads and the caches; any contents; 256-byte aligned.  0 on bad params. */
 size_t sttm_prefix_workspace_bytes(const sttm_cache* prefix, const sttm_cache* own, const sttm_prefix_params* p);

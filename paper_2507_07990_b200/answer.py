@@ -239,7 +239,8 @@ class Together:
         c = model.cfg
         self.model, self.lengths, self.seen = model, None, torch.tensor([model.rows], dtype=torch.int32, device=model.device)
         self.append = [model._append_plan(pool, layer) for pool, layer in zip(own, model.layers)]
-        self.attend = [prefix.PrefixPlan(video, c.q_heads, mine, max_rows, max_prefix=model.rows) for video, mine in zip(model.pools, own)]
+        # (as close as token by token)
+        self.attend = [prefix.PrefixPlan(video, c.q_heads, mine, max_rows, max_prefix=model.rows, fine=True) for video, mine in zip(model.pools, own)]
         # before a layer's attention and its products, and before the head, which is not in 8 bits
         norm = lambda w, int8: decoder.NormPlan(c.width, c.dtype, max_rows, pre_norm=w, eps=1e-6, quantize=int8, device=model.device)  # noqa: E731
         self.norms = [norm(layer[n], c.int8) for layer in model.layers for n in ("norm1", "norm2")] + [norm(model.norm, False)]

@@ -7,7 +7,10 @@
 // takes the row's logits out of tensor memory, forms the weights and puts them back as 16-bit operand of the second product.  The
 // reference m of the exponentials follows the row's maximum only when that has risen by more than 2^8, so O is
 // rarely rescaled; weights of up to 2^8 lose nothing in 32-bit sums.  Weights enter the product in the cache's type, rounded once (half a
-// step of it, as the output is); their sum l is taken before that rounding, in 32 bits.
+// step of it, as the output is: errors against 64 bits are 1.4 times those of the output's rounding alone); their sum l is taken before that
+// rounding, in 32 bits.  With FINE they enter as the rounded weight and what it leaves, two numbers that hold 16 bits of it (22 in fp16) as in
+// sttm_cache_attend, in the two halves of the place that the logits leave, and two products add up: 16 questions of 53 to 42 tokens on 55724 slots
+// 797 us instead of 608 (with the join), one answer token each 40.1 instead of 37.2.
 //
 // Two row blocks of 128 are in work at a time (of one block, alternate tiles), so that the products of one run beside the
 // exponentials of the other: four warps per block, three that copy (queries, then key and value tiles through a ring) and one
@@ -318,7 +321,7 @@ struct PrefixMaps {
     CUtensorMap q, k[2], v[2];    // prefix, own
 };
 
-template <typename T, int DIM>
+template <typename T, int DIM, bool FINE>
 __global__ void __launch_bounds__(PrefixShape<DIM>::THREADS, 1)
 k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ PrefixMaps maps) {
     using Shape = PrefixShape<DIM>;
@@ -612,8 +615,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tc_fence_after();
                 if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < SLOTS / 32; k++)
+                    for (int k = 0; k < SLOTS / 32; k++) {
                         mma_ts(d, tm + b * 128 + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), k > 0 ? 1 : more);
+                        if (FINE) mma_ts(d, tm + b * 128 + 64 + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), 1);
+                    }
                 }
                 __syncwarp();
                 if (!mbar_wait_near(p_full + 8 * b, weights_turn[b], timed_out)) return false;
@@ -621,8 +626,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 tc_fence_after();
                 if (elected()) {
 #pragma unroll
-                    for (int k = SLOTS / 32; k < SLOTS / 16; k++)
+                    for (int k = SLOTS / 32; k < SLOTS / 16; k++) {
                         mma_ts(d, tm + b * 128 + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), 1);
+                        if (FINE) mma_ts(d, tm + b * 128 + 64 + k * 8, v_lo + k * (2048 / 16), kOperandHigh, attend_idesc<T>(DIM, true), 1);
+                    }
                     tc_commit(o_full_u + 8 * set);
                     if (frees) tc_commit(empty_u + 8 * at);
                 }
@@ -760,7 +767,7 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                 uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int i = 0; i < SLOTS / 32; i++) {
-                    uint32_t w[16];
+                    uint32_t w[16], left_over[16];
 #pragma unroll
                     for (int k = 0; k < 16; k++) {
                         const uint64_t e = fma2(both(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), scale2, base2);
@@ -770,8 +777,13 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
                         p1 = exp2_fast(p1);
                         sum[k & 1] = add2(sum[k & 1], both(p0, p1));
                         w[k] = Pair<T>::pack(p0, p1);
+                        if constexpr (FINE) {
+                            const float2 rounded = Pair<T>::split(w[k]);
+                            left_over[k] = Pair<T>::pack(p0 - rounded.x, p1 - rounded.y);       // (the differences are exact)
+                        }
                     }
                     tmem_store16(s_at + 16 * i, w);
+                    if constexpr (FINE) tmem_store16(s_at + 64 + 16 * i, left_over);
                     if (i + 1 == SLOTS / 64) {                  // the product begins with the first half of the weights
                         tmem_wait_store();
                         tc_fence_before();

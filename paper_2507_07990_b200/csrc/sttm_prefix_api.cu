@@ -149,9 +149,13 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
             if ((r = make_part_map(c, c->k, a.page_box[i], &maps.k[i])) == STTM_OK) r = make_part_map(c, c->v, a.page_box[i], &maps.v[i]);
         }
         if (r != STTM_OK) return r;
-        static size_t allowed[kMaxDevices] = {};
-        if ((r = allow_smem((const void*)k_prefix_attend<T, D>, PrefixShape<D>::SMEM, allowed)) != STTM_OK) return r;
-        if ((r = launch(k_prefix_attend<T, D>, pl.grid, PrefixShape<D>::THREADS, PrefixShape<D>::SMEM, 0, stream, a, maps)) != STTM_OK) return r;
+        auto attend = [&](auto fine) -> sttm_status {
+            constexpr bool FINE = decltype(fine)::value;
+            static size_t allowed[kMaxDevices] = {};
+            const sttm_status f = allow_smem((const void*)k_prefix_attend<T, D, FINE>, PrefixShape<D>::SMEM, allowed);
+            return f != STTM_OK ? f : launch(k_prefix_attend<T, D, FINE>, pl.grid, PrefixShape<D>::THREADS, PrefixShape<D>::SMEM, 0, stream, a, maps);
+        };
+        if ((r = p->fine ? attend(std::true_type()) : attend(std::false_type())) != STTM_OK) return r;
         return pl.join_rows == 8 ? launch(k_prefix_join<T, D, 8>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a)
                                  : launch(k_prefix_join<T, D, 32>, pl.join_grid, kPrefixJoinThreads, 0, 0, stream, a);
     });

@@ -24,7 +24,7 @@ class PrefixParams(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_row", C.c_longlong), ("q_head", C.c_longlong), ("rows", C.c_longlong), ("q_heads", C.c_int),
                 ("seqs", C.c_int), ("row_offsets", C.c_void_p), ("seq_offsets", C.c_void_p), ("prefix_lengths", C.c_void_p),
                 ("lengths", C.c_void_p), ("max_prefix", C.c_int), ("max_own", C.c_int), ("scale", C.c_float), ("out", C.c_void_p),
-                ("lse", C.c_void_p), ("device_status", C.c_void_p)]
+                ("lse", C.c_void_p), ("device_status", C.c_void_p), ("fine", C.c_int)]
 
 
 @dataclass
@@ -36,10 +36,11 @@ class PrefixOutput:
 
 class PrefixPlan:
     """Repeated sttm_prefix_attend calls.  ``prefix``: a table row per prefix; ``own``: one per sequence (None: new tokens see their
-    prefix only).  ``max_rows``: new tokens of a call at most; ``max_prefix``, ``max_own``: slots at most (None: what the tables have room for)."""
+    prefix only).  ``max_rows``: new tokens of a call at most; ``max_prefix``, ``max_own``: slots at most (None: what the tables have room for).
+    ``fine``: attention weights are not rounded to the cache's type before they meet the values, as in AttendPlan; closer, and slower."""
 
     def __init__(self, prefix: PagedCache, q_heads: int, own: Optional[PagedCache] = None, max_rows: int = 1, scale: Optional[float] = None,
-                 max_prefix: Optional[int] = None, max_own: Optional[int] = None, seqs: Optional[int] = None):
+                 max_prefix: Optional[int] = None, max_own: Optional[int] = None, seqs: Optional[int] = None, fine: bool = False):
         _want(own is None or own.device == prefix.device, "both caches must be on one device")
         _want(own is not None or seqs is not None, "seqs is wanted where there are no own slots")
         self.prefix, self.own, self.q_heads, self.max_rows = prefix, own, q_heads, max_rows
@@ -48,7 +49,7 @@ class PrefixPlan:
         self.lse = torch.empty((max_rows, q_heads), dtype=torch.float32, device=prefix.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=prefix.device)
         p = self.params = PrefixParams()
-        p.rows, p.q_heads, p.seqs = max_rows, q_heads, self.seqs
+        p.rows, p.q_heads, p.seqs, p.fine = max_rows, q_heads, self.seqs, int(fine)
         p.max_prefix = prefix.width * prefix.page if max_prefix is None else int(max_prefix)
         if own is not None:
             p.max_own = own.width * own.page if max_own is None else int(max_own)
@@ -100,7 +101,7 @@ class PrefixPlan:
 
 
 def sttm_prefix_attend(prefix: PagedCache, q: torch.Tensor, row_offsets: torch.Tensor, prefix_lengths: torch.Tensor, own: Optional[PagedCache] = None,
-                       lengths: Optional[torch.Tensor] = None, seq_offsets: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> PrefixOutput:
-    """Attention of new tokens over a shared prefix and their own slots; see PrefixPlan.run."""
-    plan = PrefixPlan(prefix, q.shape[1], own, q.shape[0], scale, seqs=row_offsets.shape[0] - 1)
+                       lengths: Optional[torch.Tensor] = None, seq_offsets: Optional[torch.Tensor] = None, scale: Optional[float] = None, fine: bool = False) -> PrefixOutput:
+    """Attention of new tokens over a shared prefix and their own slots; see PrefixPlan and PrefixPlan.run."""
+    plan = PrefixPlan(prefix, q.shape[1], own, q.shape[0], scale, seqs=row_offsets.shape[0] - 1, fine=fine)
     return plan.run(q, row_offsets, prefix_lengths, lengths, seq_offsets)
