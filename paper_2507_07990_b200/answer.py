@@ -8,8 +8,10 @@ ids.  ``Answerer.ask`` puts several questions to it at once: they share the vide
 through the layers one by one, collecting the attention that every slot receives; the video's rows that no
 question token looks at are evicted; the answers are read from what is left.  ``Answerer.ask_together`` reads whole questions,
 of any lengths, in one go and keeps nothing of the video but the one cache that they share.  Weights are random: this shows
-the path, not a model.  Projections are plain matrix products, or with ``Config.int8`` the library's in 8 bits, and the video's own layers
-(a prefill) use torch's attention; norms, rotation, cache entry, cached attention and eviction are the library's.
+the path, not a model.  Rotation, cache entry with its norms of queries and keys, cached attention and eviction are the library's everywhere; in
+``ask_together`` the norms between blocks are too, in one pass with the residual stream and, with ``Config.int8``, the rounding to 8 bits (``watch`` and ``ask``
+take them from torch).  Projections are plain matrix products, or with ``Config.int8`` the library's in 8 bits, and the video's own layers (a prefill) use torch's
+attention.
 """
 from __future__ import annotations
 
@@ -34,7 +36,7 @@ class Config:
     page: int = 16
     theta: float = 1e6
     dtype: torch.dtype = torch.bfloat16
-    int8: bool = False           # the layers' projections in 8 bits
+    int8: bool = False           # the layers' projections in 8 bits (their weights stay in `dtype` beside it, to compare with)
 
 
 def _rms(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:

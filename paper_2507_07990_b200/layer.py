@@ -42,7 +42,7 @@ class MatmulParams(C.Structure):
 
 
 def _rows(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, index: int, what: str):
-    """Address and row stride of [rows, width] (any row stride)."""
+    """Address and row stride of [rows, width] (the call itself wants a row stride of at least width, more rows than one)."""
     if t.dtype is not dtype or t.shape != (rows, width) or t.get_device() != index:
         raise ValueError("%s must be a %s tensor %s on the plan's device" % (what, dtype, [rows, width]))
     row, col = t.stride()
@@ -125,7 +125,7 @@ class NormPlan:
         return self.last[1]
 
     def run(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, sum: Optional[torch.Tensor] = None) -> NormOutput:
-        """``x``, ``residual``, ``gate`` (a gate for every row) ``[rows, dim]`` with any row strides; ``sum``: where the residual
+        """``x``, ``residual``, ``gate`` (a gate for every row) ``[rows, dim]`` with any row strides of at least ``dim``; ``sum``: where the residual
         stream goes instead of the plan's buffer, ``residual`` itself for instance."""
         p, n, index = self.params, x.shape[0], self.index
         mine = self._outputs(n)
@@ -161,7 +161,7 @@ class QuantizePlan:
         self.last = (-1, None)
 
     def run(self, x: torch.Tensor) -> QuantRows:
-        """``x`` ``[rows, dim]`` (``[rows, 2 dim]`` when gated) with any row stride."""
+        """``x`` ``[rows, dim]`` (``[rows, 2 dim]`` when gated) with any row stride of at least that."""
         p, n = self.params, x.shape[0]
         if self.last[0] != n:
             if n > self.max_rows:
@@ -206,7 +206,7 @@ class MatmulPlan:
         self.last = (-1, None)
 
     def run(self, x: QuantRows, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """``x`` ``[rows, inner]``; returns ``[rows, outer]``, ``out`` if it is given (any row stride)."""
+        """``x`` ``[rows, inner]``; returns ``[rows, outer]``, ``out`` if it is given (any row stride of at least ``outer``)."""
         p, n = self.params, x.q.shape[0]
         p.x, p.x_row, p.x_scale = _quant_rows(x, n, self.inner, self.index, "x")
         if out is None:
