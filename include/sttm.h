@@ -422,7 +422,8 @@ sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const
  * sequence; both have the same heads, dim and dtype, and may lie in the same pools.  Sequence b's new tokens are the rows
  * row_offsets[b] ... row_offsets[b + 1] - 1, sequences seq_offsets[p] ... seq_offsets[p + 1] - 1 share prefix p (a sequence of
  * none has its own slots only).  Token i of sequence b's n new tokens sees all slots below prefix_lengths[p] and own slots
- * s < lengths[b] - n + i + 1 (its own key and value were appended before).
+ * s < lengths[b] - n + i + 1 (its own key and value were appended before; of offsets beyond the rows n counts the rows that are there, as
+ * sttm_cache_append does).
  *   out[row, h] = sum over them of softmax(scale q[row, h] . k[s, h / group]) v[s, h / group]
  * A row that sees no slot gives out = 0 and lse = -inf; rows of no sequence are left as they are.  What lies in slots behind a
  * length does not matter.  A value that is not finite in a slot below a length reaches every new token of its sequences.
@@ -433,7 +434,7 @@ typedef struct sttm_prefix_params {
     long long rows;               /* rows behind q; rows * q_heads below 2^31                      */
     int q_heads;                  /* a multiple of the cache's heads, at most 64 per KV head       */
     int seqs;
-    const int64_t* row_offsets;   /* [seqs + 1], not decreasing                                    */
+    const int64_t* row_offsets;   /* [seqs + 1], not decreasing, from 0 on                         */
     const int32_t* seq_offsets;   /* [prefix->seqs + 1], not decreasing; NULL: all share prefix 0, the only one */
     const int32_t* prefix_lengths;     /* [prefix->seqs] slots in use                              */
     const int32_t* lengths;       /* [seqs] own slots in use, the new tokens' among them (with own) */

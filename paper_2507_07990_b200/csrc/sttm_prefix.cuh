@@ -410,6 +410,10 @@ k_prefix_attend(const __grid_constant__ PrefixArgs a, const __grid_constant__ Pr
         }
         return bad;
     };
+    // (the entries' own offsets are looked at with them; without own slots those inside a prefix are no entry's)
+    if (a.own.seqs == 0)
+        for (int b = tid; b < a.seqs; b += Shape::THREADS)
+            if (a.row_offsets[b + 1] < a.row_offsets[b]) bits |= kStatusArg;
     int bad = 0;
     for (int e0 = 0; e0 < entries; e0 += Shape::THREADS) bad |= go_through(e0);
     if (blockIdx.x == 0 && bits) raise_status(a.status, bits);
