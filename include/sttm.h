@@ -425,8 +425,9 @@ sttm_status sttm_cache_evict(const sttm_cache* src, const sttm_cache* dst, const
  * s < lengths[b] - n + i + 1 (its own key and value were appended before; of offsets beyond the rows n counts the rows that are there, as
  * sttm_cache_append does).
  *   out[row, h] = sum over them of softmax(scale q[row, h] . k[s, h / group]) v[s, h / group]
- * A row that sees no slot gives out = 0 and lse = -inf; rows of no sequence are left as they are.  What lies in slots behind a
- * length does not matter.  A value that is not finite in a slot below a length reaches every new token of its sequences.
+ * A row that sees no slot gives out = 0 and lse = -inf (so does one whose logits are all -inf); rows of no sequence are left as they are.
+ * What lies in slots behind a length does not matter.  A value that is not finite in a slot below a length reaches every new token of its
+ * sequences; a key or a query that is NaN the rows that meet it, in out and in lse.
  */
 typedef struct sttm_prefix_params {
     const void* q;                /* [rows][q_heads][dim], 16-byte aligned                         */

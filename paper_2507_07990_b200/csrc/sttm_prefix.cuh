@@ -22,8 +22,8 @@
 // kPieceSteps for what it costs besides (queries in, O out).  What a CTA has of an item is a piece: O, l and m of its rows go to
 // memory, and k_prefix_join puts a row's pieces together.  One of the copy warps works the pieces out for the others.
 //
-// Measured (bf16, 28 / 4 heads of 128): 16 questions of 53 to 42 tokens on 55724 slots 0.62 to 0.64 ms, 516 to 537 us of them in the first
-// kernel (1140 to 1180 TFLOP/s at 1.6 GHz, the tensor cores busy 69 % of the time, the special-function units 66 %); one answer token
+// Measured (bf16, 28 / 4 heads of 128): 16 questions of 53 to 42 tokens on 55724 slots 0.53 ms at full clocks, 0.61 to 0.64 at the power limit; the first
+// kernel alone 516 to 537 us (1140 to 1180 TFLOP/s, the tensor cores busy 69 % of the time, the special-function units 66 %); one answer token
 // each 37 us, 3.1 TB/s (tiles at HBM's rate, then 7 us of start and end and 7 of the join).
 #pragma once
 

@@ -76,3 +76,25 @@ def test_a_whole_cache_that_is_not_a_number(dtype, dim):
         out, lse = results(p)
         assert out.isnan().all() and lse.isnan().all()
         assert slots(p["pre"], 0, length)[0].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("f16", 64), ("bf16", 256)])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("length", [130, 20000])
+def test_logits_of_minus_infinity(length, new, dtype, dim):
+    # keys at -inf in a channel where queries are 1: slots that weigh nothing, some or all of them
+    p = problem(34, dtype=dtype, dim=dim, q_heads=8, heads=4, page=64, lens=(length,), groups=(2,), new=(new, 1), held=(0, 0), own=False, spare=0)
+    p["q"][:, :, 0] = 1.0
+    p["pre"][0][..., 0] = 0.0
+    half = dict(p, lens=(length // 2,), prefix_lengths=p["prefix_lengths"] // 2)
+    k, _, table = p["pre"]
+    behind = torch.arange(length // 2, length, device="cuda")
+    k[table[0].long()[behind // 64], :, behind % 64, 0] = -math.inf
+    out, lse = results(p)
+    want, want_lse = results(half)
+    # the same weights, cut into other pieces: sums in 32 bits in another order, weights rounded against another reference, half a step each
+    step = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -10
+    assert float((out.double() - want.double()).norm() / want.double().norm()) < step and float((lse - want_lse).abs().max()) < 2.0 ** -15 * 20
+    k[..., 0] = -math.inf
+    out, lse = results(p)
+    assert not out.any() and (lse == -math.inf).all()
