@@ -464,7 +464,7 @@ sttm_status sttm_prefix_attend(const sttm_cache* prefix, const sttm_cache* own, 
  *   r = residual_scale * residual + gate * N(x; post_norm)      sum = r      out = N(r; pre_norm)
  * with N(y; w) = y / sqrt(mean y^2 + eps) * w, or y itself where w is NULL.  All but x may be left out: no residual is 0, no
  * gate 1; gate and gate_rows both count where both are given.  `out` is normed from r before it is rounded to `sum`.  q and
- * q_scale hold `out` in 8 bits (see sttm_quantize_rows).  Outputs may take the place of inputs row by row (same address and
+ * q_scale hold `out` in 8 bits (see sttm_quantize_rows; the least m is compared before the second norm's factor).  Outputs may take the place of inputs row by row (same address and
  * row stride); otherwise the memory from an output's first row to its last and that of any other array do not overlap (such calls
  * are refused, here and below).  Squares are summed in 32 bits.
  */
